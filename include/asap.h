@@ -443,6 +443,52 @@ asap_status asap_debug_mix_noalloc(const float* W_in, float* W_out, int N, int64
                                    const float* wgt, int kp1, float* consensus_out, void* cuda_stream,
                                    uint64_t wait_ns, int64_t drop_slab);
 
+/* Element types of the operators below. */
+typedef enum {
+  ASAP_F32 = 0,
+  ASAP_BF16 = 1,
+  ASAP_F16 = 2
+} asap_dtype;
+
+/* Global gradient norms and clipping, for gradients that the caller owns (the
+ * paper has no counterpart; each worker clips its own gradient before Eq. A.1's
+ * local step).  Tensor i is numel[i] (>= 0) contiguous elements of type dtypes[i]
+ * at grads[i] and belongs to group groups[i] in [0, n_groups) -- a worker, say
+ * (groups NULL: all to group 0; 1 <= n_groups <= 65536):
+ *     norms_out[k] = sqrt(sum of the squares of group k's gradients)
+ *     out[i] = grads[i] * (norms_out[k] > max_norm ? max_norm / norms_out[k] : 1)
+ * out NULL: only the norms.  out[i] == grads[i]: in place; written tensors may
+ * not overlap each other or another gradient.  Sums are carried so that neither
+ * their squares' overflow nor their underflow shows; out is rounded once.  The
+ * scale of a group whose norm is not finite is 1.  A group without elements has
+ * the norm 0.  max_norm > 0, infinity included.
+ * The arrays are host arrays, read during the call; grads, out, norms_out
+ * (n_groups floats) and the workspace (asap_clip_workspace bytes, 8-byte
+ * aligned, any contents) are device memory of the current device.  Tensors need
+ * their type's alignment; those that lie alike within 16 bytes in grads and out
+ * are moved fastest.  Calls that share a workspace must not overlap on the GPU.
+ * The same inputs give the same bits.  Async on cuda_stream (NULL: legacy default
+ * stream); it may be captured.  Allocates no device memory. */
+asap_status asap_clip_grads(int count, const void* const* grads, void* const* out, const int64_t* numel,
+                            const int32_t* dtypes, const int32_t* groups, int n_groups, float max_norm,
+                            float* norms_out, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/* The local SGD step (Eq. A.1, first line) with gradients clipped as by
+ * asap_clip_grads, on fp32 parameters that the caller owns:
+ *     params[i] = (1 - lr l2) params[i] - lr scale_k grads[i]
+ *     copies[i] = params[i], rounded to copy_dtypes[i] (ASAP_BF16 or ASAP_F16)
+ * copies may be NULL, or hold NULL for tensors without a copy.  The gradients
+ * are not changed.  A group whose norm is not finite takes no step: its
+ * parameters and copies stay as they are.  lr > 0, l2 >= 0, lr*l2 < 1; the rest
+ * as for asap_clip_grads. */
+asap_status asap_sgd_clipped(int count, float* const* params, void* const* copies, const int32_t* copy_dtypes,
+                             const void* const* grads, const int64_t* numel, const int32_t* dtypes,
+                             const int32_t* groups, int n_groups, float max_norm, float lr, float l2,
+                             float* norms_out, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/* Bytes of workspace of the two calls above.  Host only. */
+asap_status asap_clip_workspace(int n_groups, uint64_t* bytes);
+
 const char* asap_last_error(const asap_ctx* ctx);
 const char* asap_version(void);
 void asap_destroy(asap_ctx* ctx);

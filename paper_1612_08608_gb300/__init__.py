@@ -6,9 +6,11 @@ round counters.  The compute path is libasap.so (CUDA, sm_103a) behind the
 C ABI in include/asap.h; this package only marshals arguments.
 
 ``inputs`` (seeded synthetic data) imports without the CUDA library;
-``Context`` and ``build_graph`` load it on first use.
+``Context`` and ``build_graph`` load it on first use.  ``ops`` calls the
+context-free operators (large-vocabulary loss and gradient, clipping, the
+clipped SGD step) on torch tensors.
 """
-__all__ = ["Context", "AsapError", "build_graph", "load_library", "inputs"]
+__all__ = ["Context", "AsapError", "build_graph", "load_library", "inputs", "ops"]
 
 
 def __getattr__(name):

@@ -1,0 +1,142 @@
+"""Context-free operators of the C ABI (include/asap.h) on torch tensors that the
+caller owns: arguments are checked and marshalled here, every value is computed
+by libasap.so's kernels.  Calls are queued on the current stream of the tensors'
+device; outputs and workspaces that are not passed in come from torch's
+allocator.  Nothing here records autograd history."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import torch
+
+from ._lib import load_library
+from .api import AsapError
+
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _call(status: int):
+    if status != 0:
+        msg = load_library().asap_last_error(None)
+        raise AsapError(status, msg.decode() if msg else "")
+
+
+def _one_device(tensors) -> torch.device:
+    devices = {t.device for t in tensors}
+    if len(devices) != 1:
+        raise ValueError("tensors on more than one device: %s" % sorted(map(str, devices)))
+    device = devices.pop()
+    if device.type != "cuda":
+        raise ValueError("need CUDA tensors, got %s" % device)
+    return device
+
+
+def _pointers(tensors):
+    return (C.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
+
+
+def _tensor_list(name: str, tensors, like: Sequence[torch.Tensor]):
+    if len(tensors) != len(like):
+        raise ValueError("%s: %d tensors for %d gradients" % (name, len(tensors), len(like)))
+    if any(t is not None and (t.numel() != g.numel() or not t.is_contiguous()) for t, g in zip(tensors, like)):
+        raise ValueError("%s: need contiguous tensors of the gradients' sizes" % name)
+
+
+def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
+    """What asap_clip_grads and asap_sgd_clipped share, as (device, arrays, groups, n_groups, norms, workspace)."""
+    device = _one_device([*grads, *others])
+    dtypes = [DTYPE.get(g.dtype, -1) for g in grads]
+    if -1 in dtypes:
+        raise ValueError("gradients are float32, bfloat16 or float16")
+    if not all([g.is_contiguous() for g in grads]):
+        raise ValueError("need contiguous gradients")
+    T = len(grads)
+    if groups is not None:
+        if len(groups) != T:
+            raise ValueError("%d groups for %d gradients" % (len(groups), T))
+        if n_groups is None:
+            n_groups = max(groups) + 1
+        groups = (C.c_int32 * T)(*groups)
+    elif n_groups is None:
+        n_groups = 1
+    if norms is None:
+        norms = torch.empty(n_groups, dtype=torch.float32, device=device)
+    elif norms.dtype != torch.float32 or norms.shape != (n_groups,) or not norms.is_contiguous() or norms.device != device:
+        raise ValueError("norms: need %d contiguous float32 on %s" % (n_groups, device))
+    size = C.c_uint64()
+    _call(load_library().asap_clip_workspace(n_groups, C.byref(size)))
+    workspace = _workspace(workspace, size.value, device)
+    arrays = (_pointers(grads), (C.c_int64 * T)(*[g.numel() for g in grads]), (C.c_int32 * T)(*dtypes))
+    return device, arrays, groups, n_groups, norms, workspace
+
+
+def _workspace(workspace: Optional[torch.Tensor], size: int, device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous() or workspace.device != device:
+        raise ValueError("workspace: need contiguous uint8 on %s" % device)
+    return workspace
+
+
+def clip_workspace(n_groups: int = 1) -> int:
+    """Bytes of workspace of clip_grads and sgd_step."""
+    size = C.c_uint64()
+    _call(load_library().asap_clip_workspace(n_groups, C.byref(size)))
+    return size.value
+
+
+def clip_grads(grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
+               out: Optional[Sequence[torch.Tensor]] = None, groups: Optional[Sequence[int]] = None,
+               n_groups: Optional[int] = None, norms: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scales each group's gradients (a worker's, say; one group if ``groups`` is None) to a 2-norm of at most
+    ``max_norm`` and returns the norms before, float32 [n_groups].  ``out``: where the scaled gradients go (None: in
+    place).  With an infinite ``max_norm`` and no ``out`` only the norms are computed.  A group whose norm is not finite
+    is not scaled."""
+    if not grads:
+        raise ValueError("no gradients")
+    only = out is None and max_norm == float("inf")
+    if out is not None:
+        _tensor_list("out", out, grads)
+        if any(o.dtype != g.dtype for o, g in zip(out, grads)):
+            raise ValueError("out: need the gradients' types")
+    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
+                                                                                       workspace, out or ())
+    dst = None if only else ptrs if out is None else _pointers(out)
+    with torch.cuda.device(device):
+        _call(load_library().asap_clip_grads(len(grads), ptrs, dst, numel, dtypes, groups, n_groups, max_norm,
+                                             norms.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                             torch.cuda.current_stream().cuda_stream))
+    return norms
+
+
+def sgd_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: float, max_norm: float = float("inf"),
+             l2: float = 0.0, copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
+             groups: Optional[Sequence[int]] = None, n_groups: Optional[int] = None,
+             norms: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One SGD step w = (1 - lr l2) w - lr scale g on float32 ``params``, with ``scale`` as in clip_grads, and 16-bit
+    ``copies`` of the new parameters (None, or None for tensors without one).  Gradients keep their values.  A group
+    whose norm is not finite takes no step.  Returns the norms."""
+    if not grads:
+        raise ValueError("no gradients")
+    _tensor_list("params", params, grads)
+    if any(p.dtype != torch.float32 for p in params):
+        raise ValueError("params: need float32")
+    held = []
+    if copies is not None:
+        _tensor_list("copies", copies, grads)
+        held = [c for c in copies if c is not None]
+        if any(c.dtype not in (torch.bfloat16, torch.float16) for c in held):
+            raise ValueError("copies: need bfloat16 or float16")
+    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
+                                                                                       workspace, [*params, *held])
+    cptr = ctype = None
+    if copies is not None:
+        cptr = _pointers(copies)
+        ctype = (C.c_int32 * len(copies))(*[0 if c is None else DTYPE[c.dtype] for c in copies])
+    with torch.cuda.device(device):
+        _call(load_library().asap_sgd_clipped(len(grads), _pointers(params), cptr, ctype, ptrs, numel, dtypes, groups,
+                                              n_groups, max_norm, lr, l2, norms.data_ptr(), workspace.data_ptr(),
+                                              workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    return norms
