@@ -183,6 +183,8 @@ def run(s):
         if kind == "clip":
             norms = ops.clip_grads(s["grads"], s["max_norm"], out=s["out"], groups=s["group_of"])
             return s["flat"], norms
+        if "begun" not in s:          # the copies start as the parameters, as a program makes them once
+            s["begun"] = s["flat16"].copy_(s["flat"])
         norms = ops.sgd_step(s["params"], s["grads"], s["lr"], s["max_norm"], l2=s["l2"], copies=s["copies"],
                              groups=s["group_of"])
         return s["flat"], s["flat16"], norms
