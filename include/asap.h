@@ -450,6 +450,55 @@ typedef enum {
   ASAP_F16 = 2
 } asap_dtype;
 
+/* Softmax cross entropy over a large vocabulary, without keeping the logits, for
+ * N workers at once with a head each (the loss of ASAP_LOSS_SOFTMAX models, whose
+ * C is at most 1024, on features and parameters that the caller owns):
+ *     lse[i][r]  = log sum_v exp(x_r . w_v),  loss[i][r] = lse[i][r] - x_r . w_{y_r}
+ * X: N x n x d features, W: N x C x d parameters, both of type `dtype`
+ * (ASAP_BF16, ASAP_F16), in rows of ldx / ldw elements, workers stride_x /
+ * stride_w elements apart (ignored for N = 1); base addresses at multiples of
+ * 16 bytes, ld and strides multiples of 8 elements.  y: N x n class ids, packed.
+ * A row with y < 0 is left out: its loss and lse are 0, whatever X holds there;
+ * y >= C makes its loss NaN.  loss, lse: N x n floats, packed.  Products are
+ * summed in fp32, statistics kept in fp32.
+ * Limits: 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer
+ * than 10^9 tiles of 256 x 256 in N n x C, N n x d and N C x d.
+ * workspace: at least asap_xent_workspace's `least` bytes, at a multiple of 256
+ * bytes, any contents; outputs and workspace may not overlap each other or an
+ * input.  All are device memory of the current device.  Calls that share a
+ * workspace must not overlap on the GPU.  The same call gives the same bits.
+ * Async on cuda_stream (NULL: legacy default stream); it may be captured after a
+ * first call on the device.  Allocates no device memory.  The kernel's waits are
+ * time-limited (2 s); if one runs out, loss and lse are NaN and the workspace's
+ * first int32 is ASAP_ERR_TIMEOUT (else 0). */
+asap_status asap_xent_forward(int N, int64_t n, int64_t C, int64_t d, int32_t dtype, const void* X, int64_t ldx,
+                              int64_t stride_x, const void* W, int64_t ldw, int64_t stride_w, const int32_t* y,
+                              float* loss, float* lse, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/* The gradients of sum over i, r of g[i][r] loss[i][r] with respect to X and W:
+ *     R = g (softmax(X W^T) - onehot(y)),  dX = R W,  dW = R^T X
+ * lse: as asap_xent_forward gave it; g: N x n floats, packed (rows left out: not
+ * read for them).  dX: N x n x d, dW: N x C x d of type `dtype`, laid out as X and
+ * W are; either may be NULL.  The logits are computed again, a piece of the
+ * vocabulary at a time: R of one piece is held in the workspace, scaled so
+ * that the largest |g| of a worker lies at 2^14, and rounded to `dtype`; so an
+ * element of dX or dW is off by about one rounding of R's elements and one of its
+ * own.  dX rows of rows left out are 0.  A workspace of `least` bytes takes pieces
+ * of 256 columns; more makes them wider, and fewer (asap_xent_workspace's `bytes`
+ * is a good size; the width changes the order of dX's sums).  If a wait runs out,
+ * dX and dW hold a NaN and the workspace's first int32 is ASAP_ERR_TIMEOUT.  The rest
+ * as for asap_xent_forward. */
+asap_status asap_xent_backward(int N, int64_t n, int64_t C, int64_t d, int32_t dtype, const void* X, int64_t ldx,
+                               int64_t stride_x, const void* W, int64_t ldw, int64_t stride_w, const int32_t* y,
+                               const float* lse, const float* g, void* dX, int64_t lddx, int64_t stride_dx, void* dW,
+                               int64_t lddw, int64_t stride_dw, void* workspace, uint64_t workspace_bytes,
+                               void* cuda_stream);
+
+/* Bytes of workspace of asap_xent_forward (backward_pass 0) or asap_xent_backward
+ * (else): the least, and a good size.  Either may be NULL.  Host only. */
+asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int backward_pass, uint64_t* least,
+                                uint64_t* bytes);
+
 /* Global gradient norms and clipping, for gradients that the caller owns (the
  * paper has no counterpart; each worker clips its own gradient before Eq. A.1's
  * local step).  Tensor i is numel[i] (>= 0) contiguous elements of type dtypes[i]

@@ -1,0 +1,1286 @@
+// asap_xent_forward and asap_xent_backward: softmax cross entropy of z = x . w over
+// a large vocabulary, and its gradients, in pieces of the vocabulary and without
+// keeping the logits, for N workers with a head each.
+//
+//   lse_i  = log sum_v exp z_iv,  loss_i = lse_i - z_{i, y_i},  z_iv = x_i . w_v
+//   r_iv   = g_i (exp(z_iv - lse_i) - [v = y_i])
+//   dX     = R W,  dW = R^T X
+//
+// All four products run in one kernel template on the 5th-generation tensor
+// cores.  A cluster of two CTAs makes a 256 x 256 tile (tcgen05.mma, cta_group::2:
+// each CTA keeps 128 rows of the accumulator in its TMEM, and brings 128 rows of A
+// and 128 of B; a tile costs each SM a third less shared-memory reading than one of
+// 128 x 256 of its own).  Per CTA: one warp issues TMA loads into a ring of stages, one
+// (of the even CTA) the MMAs, and eight drain the other of two accumulators:
+//   logits    A = X, B = W (both K-major); a row's running maximum and sum of
+//             exponentials over 128 columns go to a table, which k_finish_loss joins.
+//             No logit is written.
+//   residual  the same product again for one piece of the vocabulary, with R as the
+//             epilogue, 16-bit, in the workspace
+//   grads     of the piece, in one launch:
+//             dX: A = R, B = W^T (MN-major): sums over the vocabulary, so a piece adds to
+//             an fp32 accumulator, and few rows split the piece over several;
+//             dW: A = R^T, B = X^T (both read MN-major from R and X as they lie)
+//
+// Rows without a label cost nothing: k_prepare lists the others, and copies X's
+// rows together if any is left out (so that what stands in the others, NaN even,
+// meets no product).  It also takes the logits of the labels, in fp32 arithmetic: the
+// tensor cores' sums are cut off after each step, which shows in the loss (d = 4096,
+// logits of 12: 3e-6 of it); k_finish_loss puts the label's term in lse right by it.  R is fp16 for fp16 operands (an MMA's have one type): it is
+// scaled by a power of two that brings the largest |g| near the top of the range.
+//
+// Every wait is time-limited.  One that runs out sets the workspace's status word; the
+// kernels after it do nothing but turn their outputs' first element into NaN.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+#include <mutex>
+
+#include "asap_internal.h"
+
+namespace asap {
+void set_thread_error(const char* msg);
+}
+
+namespace {
+
+using namespace asap;
+
+constexpr int kTile = 256;                     // rows and columns of a cluster's tile
+constexpr int kHalf = 128;                     // of a CTA's share
+constexpr int kTileK = 64;                     // 128 bytes: one swizzle row
+constexpr int kStages = 7;
+constexpr uint32_t kOperandBytes = kHalf * kTileK * 2;          // 16 KB of A, and of B
+constexpr uint32_t kStageBytes = 2 * kOperandBytes;
+constexpr uint32_t kBoxBytes = 64 * 64 * 2;                     // a TMA load: 64 x 64 elements
+constexpr int kEpiWarps = 8;                                    // two per TMEM lane quarter
+constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPairs = 76;                     // clusters that a GB300 holds: what a split is sized for
+
+constexpr int kTileSteps = 6;                  // what a tile of dX or dW takes besides its steps, in steps
+
+enum Mode { kLogits, kResidual, kGrads };
+
+// ---- PTX ------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+
+__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(bar)), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_u32(bar)), "r"(bytes)
+               : "memory");
+}
+
+// Acquires at cluster scope: arrivals come from both CTAs.
+__device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+      " selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = now_ns();
+  for (unsigned n = 1;; ++n) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((n & 63u) == 0 && now_ns() - t0 > kWaitNs) return false;
+  }
+}
+
+// The address of `p`'s place in the shared memory of cluster CTA `rank`.
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+// Into this CTA's shared memory; the bytes are counted on the even CTA's barrier.
+__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* m, uint32_t cluster_bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+      "[%5];"
+      :: "r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+      :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+}
+
+// Arrives on the barrier (of either CTA) once the MMAs issued so far are done.
+__device__ __forceinline__ void umma_commit(uint32_t cluster_bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(cluster_bar)
+               : "memory");
+}
+
+// The warp's lanes come together first: they may have parted over their rows.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Shared-memory descriptor of a tile in 128-byte swizzle.  K-major: rows of 64 k,
+// 8-row groups 1024 bytes apart.  MN-major: blocks of 64 rows or columns (8 KB apart:
+// one TMA box each), in them one 128-byte row per k, groups of 8 k 1024 bytes apart.
+// Sixteen k further is 32 bytes, or 16 rows of 128.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(mn_major ? kBoxBytes >> 4 : 1) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+// fp32 accumulator, 256 x 256; bf16 or fp16 operands.
+__device__ __forceinline__ uint32_t instr_desc(bool bf16, bool a_mn, bool b_mn) {
+  const uint32_t t = bf16 ? 1u : 0u;
+  return (1u << 4) | (t << 7) | (t << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
+         (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+}
+
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
+  uint32_t u;
+  if (bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+  return u;
+}
+
+__device__ __forceinline__ float2 unpack16(uint32_t u, bool bf16) {
+  if (bf16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+
+template <bool V>
+struct Bool {
+  static constexpr bool value = V;
+};
+
+// ---- arguments ------------------------------------------------------------------
+// A matrix of results: [N] of rows of 16-bit elements.
+struct Out {
+  uint16_t* p;
+  long long ld, stride;
+  int wide;                 // rows lie at multiples of 32 bytes
+};
+
+struct Gemm {
+  int N;
+  int n;                    // rows of X
+  int C, d;
+  int bf16;
+  int v0, width;            // piece of the vocabulary (residual, grads)
+  int tiles_v, tiles_d;     // of the piece (logits: of all), of the features
+  int splits;               // dX: parts of the piece's columns
+  int first, direct;        // dX: the piece starts the sums; the sums are dX itself
+  const int* nv;            // [N] rows with a label
+  const float* scale;       // [N] of R
+  const int* perm;          // [N][n] the rows with a label, in order
+  const int* y;             // [N][n]
+  const float* lse;         // [N][n]
+  const float* g;           // [N][n]
+  float2* part;             // logits: [N][n][2 tiles_v]
+  float* zy;                // logits: [N][n] of the labels, as summed here
+  float* acc;               // dX: [splits][N][rows][ld_acc]
+  long long acc_rows, ld_acc;
+  Out R, dX, dW;
+  int* status;
+};
+
+__device__ __forceinline__ void fail(int* status) { atomicExch(status, static_cast<int>(ASAP_ERR_TIMEOUT)); }
+
+__device__ __forceinline__ void poison(const Out& o, long long at, bool bf16) {
+  if (o.p) o.p[at] = bf16 ? 0x7fc0 : 0x7e00;
+}
+
+// The tiles that a cluster takes, the same for all its warps.
+//   logits, residual: every clusters-th of rows x vocabulary;
+//   grads: every clusters-th tile of dX; then dW's in order, dealt first to the clusters
+//   with a tile of dX less, for as long as it takes the others, and then to all.  (A
+//   piece's dX has few long tiles: 256 of 512 steps at n = d = 4096, three for
+//   most of 76 clusters, four for the rest.  dW's are many and short.)  Adjacent
+//   tiles of dW at a time share what they read: given to a cluster one behind the other, 76
+//   of them held 2 MB of R each, more than L2, and a piece took 1.7 ms, not 1.4.
+template <int M>
+struct Walk {
+  const Gemm& a;
+  int row_tiles, cluster, clusters, at, end, step;
+  int total_w, early, few;  // dW's tiles; those dealt early, to the last `few` clusters
+  int phase;                // 0, dW: 1, 2
+  bool dw;                  // the tile is one of dW
+  int worker = -1, nv = 0;
+  int m, nn, split;         // the tile
+  int k0, kt;               // its 64-wide steps
+
+  __device__ Walk(const Gemm& g, int most, bool dead, int cluster_, int clusters_) : a(g), cluster(cluster_), clusters(clusters_) {
+    row_tiles = (most + kTile - 1) / kTile;
+    dw = false;
+    phase = 0;
+    at = cluster;
+    step = clusters;
+    total_w = early = few = 0;
+    if (M != kGrads) {
+      end = dead ? 0 : a.N * row_tiles * a.tiles_v;
+      return;
+    }
+    end = dead || !a.dX.p ? 0 : a.N * row_tiles * a.tiles_d * a.splits;
+    total_w = dead || !a.dW.p ? 0 : a.N * a.tiles_v * a.tiles_d;
+    const int many = end % clusters;                            // clusters with a tile of dX more
+    few = clusters - many;
+    if (many) {
+      // Steps of a tile of dX for one of dW; a tile costs some by itself.
+      const int cost_x = (a.width + kTileK - 1) / kTileK / a.splits + kTileSteps;
+      const int cost_w = (most + kTileK - 1) / kTileK + kTileSteps;
+      const long long rounds = min(cost_x / cost_w, total_w / few);
+      early = static_cast<int>(rounds) * few;
+    }
+  }
+
+  __device__ __forceinline__ bool next() {
+    for (;;) {
+      if (at >= end) {
+        if (M != kGrads || phase == 2) return false;
+        dw = true;
+        if (++phase == 1) {
+          at = cluster - (clusters - few);
+          end = at < 0 ? at : early;
+          step = few;
+        } else {
+          at = early + cluster;
+          end = total_w;
+          step = clusters;
+        }
+        continue;
+      }
+      int t = at;
+      at += step;
+      const int tiles_n = M == kGrads ? a.tiles_d : a.tiles_v;
+      const int tiles_m = dw ? a.tiles_v : row_tiles;
+      const int plane = tiles_m * tiles_n;
+      const int parts = M == kGrads && !dw ? a.splits : 1;
+      int i = 0;
+      if (a.N > 1) {
+        i = t / (plane * parts);
+        t -= i * plane * parts;
+      }
+      if (i != worker) {
+        worker = i;
+        nv = a.nv[i];
+      }
+      split = parts > 1 ? t / plane : 0;
+      t -= split * plane;
+      // Eight tiles along one side meet all tiles of the other, so that what the
+      // clusters read at a time stays in L2.
+      const int gi = t / (8 * tiles_m), in = t - gi * 8 * tiles_m, wide = min(8, tiles_n - gi * 8);
+      m = in / wide;
+      nn = gi * 8 + (in - m * wide);
+      k0 = 0;
+      if (dw) {
+        kt = (nv + kTileK - 1) / kTileK;
+        return true;
+      }
+      if (m * kTile >= nv) continue;
+      if (M != kGrads) {
+        kt = (a.d + kTileK - 1) / kTileK;
+        return true;
+      }
+      const int k = (a.width + kTileK - 1) / kTileK;
+      k0 = static_cast<int>(static_cast<long long>(k) * split / a.splits);
+      kt = static_cast<int>(static_cast<long long>(k) * (split + 1) / a.splits) - k0;
+      if (kt > 0 || a.first) return true;
+    }
+  }
+};
+
+// tm_r: R; tm_x, tm_xc: X as it lies, and its rows with labels together; tm_w: W.
+template <int M>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_xent(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xc,
+           const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_r, const Gemm a) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* full = reinterpret_cast<uint64_t*>(base + static_cast<size_t>(kStages) * kStageBytes);   // used in the even CTA
+  uint64_t* empty = full + kStages;
+  uint64_t* acc_full = empty + kStages;                                            // [2]
+  uint64_t* acc_empty = acc_full + 2;                                              // [2], used in the even CTA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(acc_full + s, 1);
+      mbar_init(acc_empty + s, 2 * kEpiWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(tmem_slot)),
+                 "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t tmem = *tmem_slot;
+  const bool dead = *static_cast<volatile int*>(a.status) != 0;
+  if (M == kGrads && dead && blockIdx.x == 0 && threadIdx.x == 0) {
+    poison(a.dW, 0, a.bf16);
+    if (a.direct) poison(a.dX, 0, a.bf16);
+  }
+  int most = 0;                                                 // rows with a label, of any worker
+  for (int i = lane; i < a.N; i += 32) most = max(most, a.nv[i]);
+  most = __reduce_max_sync(0xffffffffu, most);
+  Walk<M> w(a, most, dead, static_cast<int>(blockIdx.x >> 1), static_cast<int>(gridDim.x >> 1));
+
+  if (warp == 0) {
+    if (lane == 0) {
+      long long g = 0;
+      bool ok = true;
+      while (ok && w.next()) {
+        const CUtensorMap* mx = w.nv == a.n ? &tm_x : &tm_xc;
+        const int a0 = w.m * kTile + static_cast<int>(rank) * kHalf;
+        const int b0 = (M != kGrads ? a.v0 : 0) + w.nn * kTile + static_cast<int>(rank) * kHalf;
+        // Both operands' boxes of a step; which of them have k for their rows is known to the compiler.
+        auto steps = [&](const CUtensorMap* ma, const CUtensorMap* mb, int ka, int kb, auto a_mn, auto b_mn) {
+          const int worker = w.worker, kt = w.kt;
+          for (int k = 0; k < kt; ++k, ++g, ka += kTileK, kb += kTileK) {
+            const int s = static_cast<int>(g % kStages);
+            if (g >= kStages && !mbar_wait(empty + s, static_cast<uint32_t>((g / kStages - 1) & 1))) return false;
+            if (rank == 0) mbar_expect_tx(full + s, 2 * kStageBytes);
+            const uint32_t bar = cluster_addr(full + s, 0);
+            unsigned char* pa = base + s * kStageBytes;
+            unsigned char* pb = pa + kOperandBytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (a_mn.value) tma_load(pa + h * kBoxBytes, ma, bar, a0 + 64 * h, ka, worker);
+              else tma_load(pa + h * kBoxBytes, ma, bar, ka, a0 + 64 * h, worker);
+              if (b_mn.value) tma_load(pb + h * kBoxBytes, mb, bar, b0 + 64 * h, kb, worker);
+              else tma_load(pb + h * kBoxBytes, mb, bar, kb, b0 + 64 * h, worker);
+            }
+          }
+          return true;
+        };
+        const int k64 = w.k0 * kTileK;
+        if (M != kGrads) ok = steps(mx, &tm_w, 0, 0, Bool<false>(), Bool<false>());
+        else if (w.dw) ok = steps(&tm_r, mx, 0, 0, Bool<true>(), Bool<true>());
+        else ok = steps(&tm_r, &tm_w, k64, a.v0 + k64, Bool<false>(), Bool<true>());
+        if (!ok) fail(a.status);
+      }
+      // No CTA leaves with a copy in flight: the last one into each stage has landed in
+      // both, as the even CTA's barriers tell; the odd one waits for it at the end.
+      if (rank == 0)
+        for (int s = 0; s < kStages && s < g; ++s)
+          if (!mbar_wait(full + s, static_cast<uint32_t>(((g - 1 - s) / kStages) & 1))) fail(a.status);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      long long g = 0;
+      int n = 0;                                                // accumulators filled
+      bool ok = true;
+      while (ok && w.next()) {
+        if (w.kt == 0) continue;
+        const int ab = n & 1;
+        if (n >= 2 && !mbar_wait(acc_empty + ab, static_cast<uint32_t>(((n >> 1) - 1) & 1))) {
+          fail(a.status);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t acc = tmem + static_cast<uint32_t>(ab) * kTile;
+        // (what the descriptors hold has to be known to the compiler)
+        auto steps = [&](auto a_mn, auto b_mn) {
+          const uint32_t idesc = instr_desc(a.bf16 != 0, a_mn.value, b_mn.value);
+          for (int k = 0; k < w.kt; ++k, ++g) {
+            const int s = static_cast<int>(g % kStages);
+            if (!mbar_wait(full + s, static_cast<uint32_t>((g / kStages) & 1))) return false;
+            tc_fence_after();
+            const uint32_t pa = smem_u32(base + s * kStageBytes), pb = pa + kOperandBytes;
+#pragma unroll
+            for (int kk = 0; kk < kTileK / 16; ++kk)
+              umma(acc, smem_desc(pa + kk * (a_mn.value ? 2048 : 32), a_mn.value),
+                   smem_desc(pb + kk * (b_mn.value ? 2048 : 32), b_mn.value), idesc, (k | kk) != 0);
+            umma_commit(cluster_addr(empty + s, 0));
+            umma_commit(cluster_addr(empty + s, 1));
+          }
+          return true;
+        };
+        if (M != kGrads) ok = steps(Bool<false>(), Bool<false>());
+        else if (w.dw) ok = steps(Bool<true>(), Bool<true>());
+        else ok = steps(Bool<false>(), Bool<true>());
+        if (!ok) fail(a.status);
+        if (ok) {
+          umma_commit(cluster_addr(acc_full + ab, 0));
+          umma_commit(cluster_addr(acc_full + ab, 1));
+        }
+        ++n;
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3, part = (warp - 2) >> 2;       // TMEM lanes; columns 128 part .. +127
+    const int r = quarter * 32 + lane;                          // row of this CTA's share
+    const uint32_t release[2] = {cluster_addr(acc_empty, 0), cluster_addr(acc_empty + 1, 0)};
+    int n = 0, seen = -1;                                       // accumulators drained; the worker of `scale`
+    float scale = 1.f, unscale = 1.f;
+    float v[32];
+    // 32 columns of this thread's row as 16-bit values, the first `left` of them: whole
+    // sectors where the rows lie at multiples of 32 bytes (wide), else groups of 16.
+    auto to_memory = [&](uint16_t* o, int left, bool wide) {
+      uint32_t u[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) u[j] = pack16(v[2 * j], v[2 * j + 1], a.bf16);
+      if (left >= 32 && wide) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                       :: "l"(o + 16 * q), "r"(u[8 * q]), "r"(u[8 * q + 1]), "r"(u[8 * q + 2]), "r"(u[8 * q + 3]),
+                          "r"(u[8 * q + 4]), "r"(u[8 * q + 5]), "r"(u[8 * q + 6]), "r"(u[8 * q + 7]) : "memory");
+        return;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (left >= 8 * q + 8) {
+          *reinterpret_cast<uint4*>(o + 8 * q) = make_uint4(u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (left > 8 * q + e) o[8 * q + e] = static_cast<uint16_t>(u[4 * q + (e >> 1)] >> (16 * (e & 1)));
+        }
+      }
+    };
+    while (w.next()) {
+      const int row = w.m * kTile + static_cast<int>(rank) * kHalf + r;   // of the tile's matrix
+      const int col0 = w.nn * kTile + part * kHalf;                       // this thread's first column
+      const long long wn = static_cast<long long>(w.worker) * a.n;
+      const bool live = !w.dw && row < w.nv;
+      if (M != kLogits && w.worker != seen) {
+        seen = w.worker;
+        scale = a.scale[seen];
+        unscale = 1.f / scale;
+      }
+      // What a row needs is fetched while its products are still summed.
+      int at = 0, yb = -1;
+      float off = 0.f, gs = 0.f;
+      if (live && (M != kGrads || a.direct)) at = a.perm[wn + row];
+      if (live && M != kGrads) yb = a.y[wn + at] - a.v0;
+      if (live && M == kResidual) {
+        off = -a.lse[wn + at] * kLog2e;
+        gs = a.g[wn + at] * scale;
+      }
+      const int ab = n & 1;
+      if (w.kt > 0) {
+        // All threads of a half go on or give up together: they meet at its barrier.
+        const bool ok = mbar_wait(acc_full + ab, static_cast<uint32_t>((n >> 1) & 1));
+        uint32_t bad;
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+            : "=r"(bad) : "r"(static_cast<uint32_t>(!ok)), "r"(1 + part) : "memory");
+        if (bad) {
+          fail(a.status);
+          if (M == kGrads && lane == 0 && warp == 2 && rank == 0) {
+            const long long col = static_cast<long long>(w.nn) * kTile;
+            if (w.dw) poison(a.dW, w.worker * a.dW.stride + (a.v0 + static_cast<long long>(w.m) * kTile) * a.dW.ld + col, a.bf16);
+            else if (a.direct) poison(a.dX, w.worker * a.dX.stride + static_cast<long long>(a.perm[wn + w.m * kTile]) * a.dX.ld + col, a.bf16);
+          }
+          break;
+        }
+        tc_fence_after();
+      }
+      const uint32_t trow = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(ab) * kTile +
+                            static_cast<uint32_t>(part) * kHalf;
+      if (M == kLogits) {
+        float m = -INFINITY, s = 0.f, zy = 0.f;
+        bool mine = false;
+        for (int c = 0; c < 4; ++c) {
+          const int cc = col0 + 32 * c;
+          if (cc >= a.C) break;
+          tmem_ld32(trow + 32 * c, v);
+          if (cc + 32 > a.C) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (cc + j >= a.C) v[j] = -INFINITY;
+          }
+          if (yb >= cc && yb < cc + 32) {
+            mine = true;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (cc + j == yb) zy = v[j];
+          }
+          float cm = m;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) cm = fmaxf(cm, v[j]);
+          // Nothing but -inf so far adds nothing; NaN goes on in the sum.
+          const float mm = cm == -INFINITY ? 0.f : cm;
+          const float top = -mm * kLog2e;
+          s *= ex2(fmaf(m, kLog2e, top));
+          float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            s0 += ex2(fmaf(v[j], kLog2e, top));
+            s1 += ex2(fmaf(v[j + 1], kLog2e, top));
+            s2 += ex2(fmaf(v[j + 2], kLog2e, top));
+            s3 += ex2(fmaf(v[j + 3], kLog2e, top));
+          }
+          s += (s0 + s1) + (s2 + s3);
+          m = cm;
+        }
+        if (live) {
+          a.part[(wn + row) * (2 * a.tiles_v) + 2 * w.nn + part] = make_float2(m, s);
+          if (mine) a.zy[wn + row] = zy;
+        }
+      } else if (M == kResidual) {
+        uint16_t* out = a.R.p + w.worker * a.R.stride + static_cast<long long>(row) * a.R.ld;
+        for (int c = 0; c < 4; ++c) {
+          const int cc = col0 + 32 * c;
+          if (cc >= a.width) break;
+          tmem_ld32(trow + 32 * c, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float p = ex2(fmaf(v[j], kLog2e, off)) - (cc + j == yb ? 1.f : 0.f);
+            v[j] = live && cc + j < a.width ? gs * p : 0.f;
+          }
+          to_memory(out + cc, 32, true);                             // rows of R end at a multiple of 256 columns
+        }
+      } else {
+        const bool sums = !w.dw && !a.direct;
+        const bool stored = w.dw ? a.v0 + row < a.C : live;
+        uint16_t* out = w.dw ? a.dW.p + w.worker * a.dW.stride + (a.v0 + static_cast<long long>(row)) * a.dW.ld
+                             : a.dX.p + w.worker * a.dX.stride + static_cast<long long>(at) * a.dX.ld;
+        const bool wide = w.dw ? a.dW.wide : a.dX.wide;
+        float* acc = a.acc + ((static_cast<long long>(w.split) * a.N + w.worker) * a.acc_rows + row) * a.ld_acc;
+        for (int c = 0; c < 4; ++c) {
+          const int cc = col0 + 32 * c;
+          if (cc >= a.d) break;
+          if (w.kt > 0) {
+            tmem_ld32(trow + 32 * c, v);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+          }
+          if (!stored) continue;
+          if (!sums) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= unscale;
+            to_memory(out + cc, a.d - cc, wide);
+            continue;
+          }
+          float4* o = reinterpret_cast<float4*>(acc + cc);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            if (cc + 4 * u >= a.ld_acc) break;
+            float4 x = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+            if (!a.first) {
+              const float4 p = o[u];
+              x.x += p.x;
+              x.y += p.y;
+              x.z += p.z;
+              x.w += p.w;
+            }
+            o[u] = x;
+          }
+        }
+      }
+      if (w.kt > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_at(release[ab]);
+        ++n;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// ---- before: the rows with a label ---------------------------------------------------
+constexpr int kPrepThreads = 256;
+constexpr int kPrepBlocks = 512;            // per worker, at most
+
+struct Prep {
+  int N, n, C, d, bf16, per_block;
+  const uint16_t* X;
+  long long ldx, sx;
+  const uint16_t* W;        // forward: for the logits of the labels
+  long long ldw, sw;
+  float* zy;                // [N][n], by place in perm
+  const int* y;
+  const float* g;           // backward: the largest |g| sets the scale of R
+  uint16_t* Xc;             // [N][rows][ldc]
+  long long rows, ldc;
+  int* perm;
+  int* nv;
+  float* scale;
+  float* loss;              // forward
+  float* lse;
+  uint16_t* dX;             // backward
+  long long lddx, sdx;
+  int* status;
+};
+
+__device__ __forceinline__ bool labelled(int y, int C) { return y >= 0 && y < C; }
+
+// Each block takes per_block rows of a worker, 32 at a time, and counts the labels of
+// them all for itself: no other kernel has to come first.
+__global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
+  __shared__ int s_total[kPrepThreads / 32], s_before[kPrepThreads / 32];
+  __shared__ float s_max[kPrepThreads / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int worker = blockIdx.y, begin = blockIdx.x * a.per_block, end = min(begin + a.per_block, a.n);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long wn = static_cast<long long>(worker) * a.n;
+  const int* y = a.y + wn;
+  const float* g = a.g ? a.g + wn : nullptr;
+  int total = 0, before = 0;
+  float top = 0.f;
+  for (int i = tid; i < a.n; i += kPrepThreads) {
+    const int in = labelled(y[i], a.C) ? 1 : 0;
+    total += in;
+    if (i < begin) before += in;
+    if (g && in) top = fmaxf(top, fabsf(g[i]));
+  }
+  total = __reduce_add_sync(0xffffffffu, total);
+  before = __reduce_add_sync(0xffffffffu, before);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) {
+    s_total[warp] = total;
+    s_before[warp] = before;
+    s_max[warp] = top;
+  }
+  __syncthreads();
+  int nv = 0, first = 0;
+  for (int w = 0; w < kPrepThreads / 32; ++w) {
+    nv += s_total[w];
+    first += s_before[w];
+    top = fmaxf(top, s_max[w]);
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    a.nv[worker] = nv;
+    // The largest |g| becomes the largest value below 2^14 that R's type holds: what has no
+    // part of p takes no rounding then, and what is near it the smallest.
+    float sc = 1.f;
+    if (g && top > 0.f && top < INFINITY) sc = (a.bf16 ? 16320.f : 16376.f) / fmaxf(top, 1e-30f);
+    a.scale[worker] = sc;
+    if (worker == 0) *a.status = 0;
+  }
+  for (int r0 = begin; r0 < end; r0 += 32) {
+    // each warp has the 32 rows in its lanes, and takes every eighth
+    const int row = r0 + lane;
+    const int yr = row < end ? y[row] : -1;
+    const bool in = labelled(yr, a.C);
+    const unsigned rows_in = __ballot_sync(0xffffffffu, in);
+    const int place = __popc(rows_in & ((1u << lane) - 1u));
+    if (warp == 0) {
+      if (in) {
+        a.perm[wn + first + place] = row;
+      } else if (row < end && a.loss) {
+        a.loss[wn + row] = yr < 0 ? 0.f : __int_as_float(0x7fc00000);
+        a.lse[wn + row] = 0.f;
+      }
+    }
+    for (int q = warp; q < 32; q += kPrepThreads / 32) {
+      if (r0 + q >= end) break;
+      const int label = __shfl_sync(0xffffffffu, yr, q), at = first + __shfl_sync(0xffffffffu, place, q);
+      if (!((rows_in >> q) & 1u)) {
+        if (a.dX) {
+          uint16_t* dst = a.dX + worker * a.sdx + (r0 + q) * a.lddx;
+          for (int v = lane; v < a.d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = make_uint4(0u, 0u, 0u, 0u);
+          const int c = a.d / 8 * 8 + lane;
+          if (c < a.d) dst[c] = 0;
+        }
+        continue;
+      }
+      const uint16_t* x = a.X + worker * a.sx + (r0 + q) * a.ldx;
+      if (nv < a.n) {
+        uint16_t* dst = a.Xc + (worker * a.rows + at) * a.ldc;
+        for (int v = lane; v < a.d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = reinterpret_cast<const uint4*>(x)[v];
+        const int c = a.d / 8 * 8 + lane;
+        if (c < a.d) dst[c] = x[c];
+      }
+      if (a.zy) {
+        const uint16_t* w = a.W + worker * a.sw + label * a.ldw;
+        float z = 0.f;
+#pragma unroll 4
+        for (int v = lane; v < a.d / 8; v += 32) {
+          const uint4 p = reinterpret_cast<const uint4*>(x)[v], r = reinterpret_cast<const uint4*>(w)[v];
+          const float2 x0 = unpack16(p.x, a.bf16), x1 = unpack16(p.y, a.bf16), x2 = unpack16(p.z, a.bf16),
+                       x3 = unpack16(p.w, a.bf16);
+          const float2 w0 = unpack16(r.x, a.bf16), w1 = unpack16(r.y, a.bf16), w2 = unpack16(r.z, a.bf16),
+                       w3 = unpack16(r.w, a.bf16);
+          z += (fmaf(x0.x, w0.x, x0.y * w0.y) + fmaf(x1.x, w1.x, x1.y * w1.y)) +
+               (fmaf(x2.x, w2.x, x2.y * w2.y) + fmaf(x3.x, w3.x, x3.y * w3.y));
+        }
+        const int c = a.d / 8 * 8 + lane;
+        if (c < a.d) z = fmaf(unpack16(x[c], a.bf16).x, unpack16(w[c], a.bf16).x, z);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        if (lane == 0) a.zy[wn + at] = z;
+      }
+    }
+    first += __popc(rows_in);
+  }
+  // what a last step of 64 rows reads beyond the rows that were copied
+  if (nv < a.n && blockIdx.x == gridDim.x - 1)
+    for (int q = nv + warp; q < (nv + kTileK - 1) / kTileK * kTileK; q += kPrepThreads / 32) {
+      uint16_t* dst = a.Xc + (worker * a.rows + q) * a.ldc;
+      for (int c = lane; c < a.d; c += 32) dst[c] = 0;
+    }
+}
+
+// ---- after ---------------------------------------------------------------------------
+constexpr int kLossWarps = 4;
+
+// A warp joins a row's parts.
+__global__ void __launch_bounds__(kLossWarps * 32)
+    k_finish_loss(const float2* part, int slots, const float* zy, const float* zy_sum, const int* perm, const int* nv, int n,
+                  float* loss, float* lse, const int* status) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int worker = blockIdx.y, lane = threadIdx.x & 31, row = blockIdx.x * kLossWarps + (threadIdx.x >> 5);
+  const long long wn = static_cast<long long>(worker) * n;
+  if (row >= nv[worker]) return;
+  part += (wn + row) * slots;
+  float m = -INFINITY, s = 0.f;
+  auto join = [&](float pm, float ps) {
+    const float t = fmaxf(m, pm);
+    if (t > -INFINITY) s = s * ex2((m - t) * kLog2e) + ps * ex2((pm - t) * kLog2e);
+    else s += ps;                                               // 0, or NaN
+    m = t;
+  };
+#pragma unroll 4
+  for (int q = lane; q < slots; q += 32) join(part[q].x, part[q].y);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float pm = __shfl_xor_sync(0xffffffffu, m, o), ps = __shfl_xor_sync(0xffffffffu, s, o);
+    join(pm, ps);
+  }
+  if (lane != 0) return;
+  const bool dead = *static_cast<const volatile int*>(status) != 0;
+  // The label's own term, the largest of a confident row, is taken with its exact logit:
+  // d lse / d z_y = p_y.
+  const float z = zy[wn + row], off = z - zy_sum[wn + row];
+  float l = dead ? __int_as_float(0x7fc00000) : m + logf(s);
+  if (fabsf(off) < 1e-2f) l += ex2((z - l) * kLog2e) * off;      // no correction of what is not finite
+  const int at = perm[wn + row];
+  lse[wn + at] = l;
+  loss[wn + at] = l - z;
+}
+
+// dX of the rows with a label from the splits' sums.
+__global__ void __launch_bounds__(256)
+    k_finish_dx(const float* acc, int splits, int N, long long rows, long long ld, const int* perm, const int* nv,
+                const float* scale, int n, int d, int bf16, uint16_t* dX, long long lddx, long long sdx, const int* status) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int worker = blockIdx.z;
+  if (*static_cast<const volatile int*>(status) != 0) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && worker == 0 && threadIdx.x == 0) dX[0] = bf16 ? 0x7fc0 : 0x7e00;
+    return;
+  }
+  const float unscale = 1.f / scale[worker];
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4;
+  if (c >= d) return;
+  for (int row = blockIdx.x; row < nv[worker]; row += gridDim.x) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < splits; ++s) {
+      const float4 p = *reinterpret_cast<const float4*>(acc + ((static_cast<long long>(s) * N + worker) * rows + row) * ld + c);
+      x.x += p.x;
+      x.y += p.y;
+      x.z += p.z;
+      x.w += p.w;
+    }
+    uint16_t* o = dX + worker * sdx + static_cast<long long>(perm[static_cast<long long>(worker) * n + row]) * lddx + c;
+    const uint2 q = make_uint2(pack16(x.x * unscale, x.y * unscale, bf16), pack16(x.z * unscale, x.w * unscale, bf16));
+    if (c + 4 <= d) *reinterpret_cast<uint2*>(o) = q;            // rows start at multiples of 16 bytes
+    else
+      for (int e = 0; c + e < d; ++e) o[e] = static_cast<uint16_t>((e < 2 ? q.x : q.y) >> (16 * (e & 1)));
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------
+asap_status reject(asap_status s, const char* msg) {
+  set_thread_error(msg);
+  return s;
+}
+
+asap_status cuda_error(const char* what, cudaError_t e) {
+  cudaGetLastError();
+  char msg[200];
+  snprintf(msg, sizeof(msg), "%s: %s", what, cudaGetErrorString(e));
+  return reject(ASAP_ERR_CUDA, msg);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct Device {
+  bool ready = false;
+  int clusters = 0;
+  EncodeTiledFn encode = nullptr;
+};
+
+constexpr int kMaxDevices = 64;
+std::mutex g_mu;
+Device g_devices[kMaxDevices];
+
+template <int M>
+cudaError_t configure() {
+  return cudaFuncSetAttribute(k_xent<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+}
+
+asap_status device(Device* out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error("no usable current device", e);
+  if (dev < 0 || dev >= kMaxDevices) return reject(ASAP_ERR_CUDA, "no usable current device");
+  std::lock_guard<std::mutex> lock(g_mu);
+  Device& d = g_devices[dev];
+  if (!d.ready) {
+    void* enc = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &enc, 12000, cudaEnableDefault, &q);
+    if (e != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      return reject(ASAP_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    if ((e = configure<kLogits>()) != cudaSuccess || (e = configure<kResidual>()) != cudaSuccess ||
+        (e = configure<kGrads>()) != cudaSuccess)
+      return cuda_error("configuring the kernels", e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, k_xent<kLogits>, &cfg);
+    if (e != cudaSuccess || n < 1) return cuda_error("no cluster of the kernel fits on the device", e);
+    d.clusters = n;
+    d.encode = reinterpret_cast<EncodeTiledFn>(enc);
+    d.ready = true;
+  }
+  *out = d;
+  return ASAP_OK;
+}
+
+// [N][rows][inner] of 16-bit elements; boxes of 64 x 64, 128-byte swizzle.
+bool encode(const Device& dev, CUtensorMap* m, bool bf16, const void* base, long long inner, long long rows, long long N,
+            long long ld, long long stride) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(N)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(stride) * 2};
+  const cuuint32_t box[3] = {64, 64, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return dev.encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                    const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline long long up(long long v, long long a) { return (v + a - 1) / a * a; }
+
+constexpr long long kMaxRows = 1 << 24, kMaxVocab = 1 << 28, kMaxD = 1 << 20;
+constexpr int kMaxWorkers = 1024;
+
+// Where everything lies in the workspace, and how the vocabulary is cut.
+struct Plan {
+  long long n_pad, ldc, ld_acc;
+  int tiles_m, tiles_v, tiles_d, splits;
+  size_t nv, scale, perm, xc, part, zy, R, acc, end;
+  long long piece;              // columns of R: all pieces but the last are as wide
+  bool direct;
+};
+
+struct Shape {
+  int N;
+  long long n, C, d;
+};
+
+bool sizes_ok(const Shape& s) {
+  if (!(s.N >= 1 && s.N <= kMaxWorkers && s.n >= 0 && s.n <= kMaxRows && s.C >= 1 && s.C <= kMaxVocab && s.d >= 1 && s.d <= kMaxD))
+    return false;
+  // tiles are counted in 32 bits (a split of dX's is at most a cluster's worth more)
+  const double m = s.n / 256 + 1, v = static_cast<double>(s.C / 256 + 1), d = static_cast<double>(s.d / 256 + 1);
+  return s.N * std::max(std::max(m * v, m * d), v * d) < 1e9;
+}
+
+size_t take(size_t& at, size_t bytes) {
+  const size_t here = at;
+  at = (at + bytes + 1023) & ~static_cast<size_t>(1023);
+  return here;
+}
+
+Plan plan_common(const Shape& s) {
+  Plan p = {};
+  p.n_pad = up(s.n, kTile);
+  p.ldc = up(s.d, 8);
+  p.ld_acc = up(s.d, 4);
+  p.tiles_m = static_cast<int>(p.n_pad / kTile);
+  p.tiles_v = static_cast<int>(up(s.C, kTile) / kTile);
+  p.tiles_d = static_cast<int>(up(s.d, kTile) / kTile);
+  size_t at = 1024;             // the status word
+  p.nv = take(at, 4 * static_cast<size_t>(s.N));
+  p.scale = take(at, 4 * static_cast<size_t>(s.N));
+  p.perm = take(at, 4 * static_cast<size_t>(s.N) * s.n);
+  p.xc = take(at, 2 * static_cast<size_t>(s.N) * p.n_pad * p.ldc);
+  p.end = at;
+  return p;
+}
+
+Plan plan_forward(const Shape& s) {
+  Plan p = plan_common(s);
+  p.part = take(p.end, 8 * static_cast<size_t>(s.N) * 2 * p.tiles_v * s.n);
+  p.zy = take(p.end, 8 * static_cast<size_t>(s.N) * s.n);
+  return p;
+}
+
+// The width of R's pieces by the bytes that there are: 0 asks for the best, 1 for the least.
+constexpr size_t kRBytes = 256u << 20;
+Plan plan_backward(const Shape& s, size_t bytes) {
+  Plan p = plan_common(s);
+  const long long whole = up(s.C, kTile);
+  const size_t column = 2 * static_cast<size_t>(s.N) * p.n_pad;
+  // dX sums over the vocabulary.  Enough tiles for every cluster: one split; else as
+  // many as give each cluster one, of eight steps at least.
+  const long long units = static_cast<long long>(s.N) * p.tiles_m * p.tiles_d;
+  p.splits = 1;
+  if (units > 0 && units < kPairs)
+    p.splits = static_cast<int>(std::max<long long>(1, std::min<long long>(kPairs / units, up(s.C, kTileK) / kTileK / 8)));
+  const size_t acc = 4 * static_cast<size_t>(p.splits) * s.N * p.n_pad * p.ld_acc;
+  auto end = [&](long long piece, bool direct) {
+    size_t at = p.end;
+    take(at, column * piece);
+    if (!direct) take(at, acc);
+    return at;
+  };
+  if (!bytes) bytes = std::max(end(kTile, false), end(0, false) + kRBytes);
+  // one piece, and dX from it as it is; also where the least that pieces need is no less
+  p.direct = p.splits == 1 && (end(whole, true) <= bytes || end(whole, true) <= end(kTile, false));
+  p.piece = whole;
+  if (!p.direct) {
+    const size_t fixed = end(0, false);
+    if (column) p.piece = static_cast<long long>(std::min(static_cast<size_t>(whole), (bytes > fixed ? bytes - fixed : 0) / column));
+    p.piece = std::max<long long>(kTile, p.piece / kTile * kTile);
+    const long long pieces = (whole + p.piece - 1) / p.piece;
+    p.piece = up((whole + pieces - 1) / pieces, kTile);           // all about as wide
+  }
+  p.R = take(p.end, column * p.piece);
+  if (!p.direct) p.acc = take(p.end, acc);
+  return p;
+}
+
+struct Matrix {
+  const void* p;
+  long long ld, stride;
+};
+
+bool matrix_ok(const Matrix& m, long long rows, long long d, int N) {
+  return (reinterpret_cast<uintptr_t>(m.p) & 15u) == 0 && m.ld >= d && m.ld % 8 == 0 && m.ld <= (1LL << 32) &&
+         (N == 1 || (m.stride % 8 == 0 && m.stride >= rows * m.ld - (m.ld - d) && m.stride <= (1LL << 38)));
+}
+
+long long stride_of(const Matrix& m, long long rows, int N) { return N == 1 ? std::max(8LL, rows * m.ld) : m.stride; }
+
+bool is_wide(const Matrix& m, int N) {
+  return ((reinterpret_cast<uintptr_t>(m.p) | static_cast<uintptr_t>(m.ld * 2) | static_cast<uintptr_t>(N == 1 ? 0 : m.stride * 2)) & 31u) == 0;
+}
+
+// The bytes from the first to behind the last element.
+struct Extent {
+  uintptr_t begin, end;
+};
+
+Extent extent(const Matrix& m, long long rows, long long d, int N) {
+  const uintptr_t b = reinterpret_cast<uintptr_t>(m.p);
+  if (!m.p || rows == 0) return {b, b};
+  return {b, b + 2 * static_cast<uintptr_t>((N - 1) * (N == 1 ? 0 : m.stride) + (rows - 1) * m.ld + d)};
+}
+
+Extent extent(const void* p, unsigned long long bytes) {
+  const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+  return {b, p ? b + static_cast<uintptr_t>(bytes) : b};
+}
+
+// Any of the first `written` meets another one.
+bool meet(const Extent* e, int count, int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = 0; j < count; ++j)
+      if (i != j && (j >= written || j > i) && e[i].begin < e[j].end && e[j].begin < e[i].end) return true;
+  return false;
+}
+
+struct Launch {
+  cudaStream_t stream;
+  bool chained = false;         // a kernel of this call is before it
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg;
+
+  cudaLaunchConfig_t* at(dim3 grid, int threads, size_t smem, bool pair) {
+    cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    int n = 0;
+    if (pair) {
+      attr[n].id = cudaLaunchAttributeClusterDimension;
+      attr[n].val.clusterDim.x = 2;
+      attr[n].val.clusterDim.y = 1;
+      attr[n].val.clusterDim.z = 1;
+      ++n;
+    }
+    if (chained) {
+      attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      attr[n].val.programmaticStreamSerializationAllowed = 1;
+      ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    chained = true;
+    return &cfg;
+  }
+};
+
+template <int M>
+cudaError_t launch_gemm(Launch& l, const Device& dev, const Gemm& a, long long tiles, const CUtensorMap& tx,
+                        const CUtensorMap& txc, const CUtensorMap& tw, const CUtensorMap& tr) {
+  const int clusters = static_cast<int>(std::min<long long>(tiles, dev.clusters));
+  return cudaLaunchKernelEx(l.at(dim3(2 * clusters), kThreads, kSmemBytes, true), k_xent<M>, tx, txc, tw, tr, a);
+}
+
+cudaError_t launch_prepare(Launch& l, Prep q) {
+  // a row for each warp while there are few
+  const int rows = (q.n + kPrepBlocks - 1) / kPrepBlocks;
+  q.per_block = rows <= 8 ? 8 : static_cast<int>(up(rows, 32));
+  return cudaLaunchKernelEx(l.at(dim3((q.n + q.per_block - 1) / q.per_block, q.N), kPrepThreads, 0, false), k_prepare, q);
+}
+
+#define XENT_CHECK(f)                                                                                             \
+  if (!sizes_ok(s))                                                                                               \
+    return reject(ASAP_ERR_ARG, f ": need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256");       \
+  if (dtype != ASAP_BF16 && dtype != ASAP_F16) return reject(ASAP_ERR_ARG, f ": need ASAP_BF16 or ASAP_F16");
+
+asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W, const int32_t* y, float* loss, float* lse,
+                    void* ws, uint64_t ws_bytes, cudaStream_t stream) {
+  XENT_CHECK("asap_xent_forward")
+  if (s.n == 0) return ASAP_OK;
+  if (!X.p || !W.p || !y || !loss || !lse || !ws) return reject(ASAP_ERR_ARG, "asap_xent_forward: NULL pointer");
+  if (!matrix_ok(X, s.n, s.d, s.N) || !matrix_ok(W, s.C, s.d, s.N))
+    return reject(ASAP_ERR_ARG, "asap_xent_forward: need X and W at multiples of 16 bytes, in rows of ld >= d elements "
+                                "and strides that are multiples of 8 elements");
+  const unsigned long long rows4 = 4ull * s.N * s.n;
+  const Extent used[] = {extent(loss, rows4), extent(lse, rows4), extent(ws, ws_bytes), extent(X, s.n, s.d, s.N),
+                         extent(W, s.C, s.d, s.N), extent(y, rows4)};
+  if (meet(used, 6, 3)) return reject(ASAP_ERR_ARG, "asap_xent_forward: outputs or workspace overlap each other or an input");
+  const Plan p = plan_forward(s);
+  if (ws_bytes < p.end || (reinterpret_cast<uintptr_t>(ws) & 255u))
+    return reject(ASAP_ERR_ARG, "asap_xent_forward: workspace too small or not at a multiple of 256 bytes");
+  Device dev;
+  const asap_status st = device(&dev);
+  if (st != ASAP_OK) return st;
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  const bool bf16 = dtype == ASAP_BF16;
+  CUtensorMap tx, txc, tw;
+  if (!encode(dev, &tx, bf16, X.p, s.d, s.n, s.N, X.ld, stride_of(X, s.n, s.N)) ||
+      !encode(dev, &txc, bf16, w + p.xc, s.d, p.n_pad, s.N, p.ldc, p.n_pad * p.ldc) ||
+      !encode(dev, &tw, bf16, W.p, s.d, s.C, s.N, W.ld, stride_of(W, s.C, s.N)))
+    return reject(ASAP_ERR_CUDA, "asap_xent_forward: cuTensorMapEncodeTiled failed");
+  Prep q = {};
+  q.N = s.N, q.n = static_cast<int>(s.n), q.C = static_cast<int>(s.C), q.d = static_cast<int>(s.d);
+  q.X = static_cast<const uint16_t*>(X.p), q.ldx = X.ld, q.sx = s.N == 1 ? 0 : X.stride;
+  q.W = static_cast<const uint16_t*>(W.p), q.ldw = W.ld, q.sw = s.N == 1 ? 0 : W.stride;
+  q.zy = reinterpret_cast<float*>(w + p.zy), q.bf16 = bf16;
+  q.y = y, q.Xc = reinterpret_cast<uint16_t*>(w + p.xc), q.rows = p.n_pad, q.ldc = p.ldc;
+  q.perm = reinterpret_cast<int*>(w + p.perm), q.nv = reinterpret_cast<int*>(w + p.nv);
+  q.scale = reinterpret_cast<float*>(w + p.scale), q.loss = loss, q.lse = lse, q.status = static_cast<int*>(ws);
+  Gemm a = {};
+  a.N = s.N, a.n = q.n, a.C = q.C, a.d = q.d, a.bf16 = bf16, a.width = q.C;
+  a.tiles_v = p.tiles_v, a.tiles_d = p.tiles_d, a.splits = 1;
+  a.nv = q.nv, a.scale = q.scale, a.perm = q.perm, a.y = y;
+  a.part = reinterpret_cast<float2*>(w + p.part), a.zy = q.zy + s.N * s.n, a.status = q.status;
+  Launch l;
+  l.stream = stream;
+  cudaError_t e = launch_prepare(l, q);
+  if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw);
+  if (e == cudaSuccess)
+    e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
+                           static_cast<const float2*>(a.part), 2 * p.tiles_v, static_cast<const float*>(q.zy), static_cast<const float*>(a.zy), a.perm, a.nv,
+                           a.n, loss, lse, static_cast<const int*>(a.status));
+  return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
+}
+
+asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W, const int32_t* y, const float* lse,
+                     const float* g, const Matrix& dX, const Matrix& dW, void* ws, uint64_t ws_bytes, cudaStream_t stream) {
+  XENT_CHECK("asap_xent_backward")
+  if (s.n > 0 && (!X.p || !W.p || !y || !lse || !g || !ws))
+    return reject(ASAP_ERR_ARG, "asap_xent_backward: NULL pointer");
+  if (!dX.p && !dW.p) return reject(ASAP_ERR_ARG, "asap_xent_backward: neither dX nor dW");
+  if ((s.n > 0 && (!matrix_ok(X, s.n, s.d, s.N) || !matrix_ok(W, s.C, s.d, s.N))) || (dX.p && !matrix_ok(dX, s.n, s.d, s.N)) ||
+      (dW.p && !matrix_ok(dW, s.C, s.d, s.N)))
+    return reject(ASAP_ERR_ARG, "asap_xent_backward: need X, W, dX and dW at multiples of 16 bytes, in rows of ld >= d "
+                                "elements and strides that are multiples of 8 elements");
+  const unsigned long long rows4 = 4ull * s.N * s.n;
+  const Extent used[] = {extent(dX, s.n, s.d, s.N), extent(dW, s.C, s.d, s.N), extent(ws, ws_bytes), extent(X, s.n, s.d, s.N),
+                         extent(W, s.C, s.d, s.N), extent(y, rows4), extent(lse, rows4), extent(g, rows4)};
+  if (meet(used, 8, 3)) return reject(ASAP_ERR_ARG, "asap_xent_backward: outputs or workspace overlap each other or an input");
+  const bool bf16 = dtype == ASAP_BF16;
+  if (s.n == 0) {
+    for (int i = 0; dW.p && i < s.N; ++i) {
+      const cudaError_t e = cudaMemset2DAsync(const_cast<char*>(static_cast<const char*>(dW.p)) + 2 * i * dW.stride,
+                                              static_cast<size_t>(dW.ld) * 2, 0, static_cast<size_t>(s.d) * 2,
+                                              static_cast<size_t>(s.C), stream);
+      if (e != cudaSuccess) return cuda_error("asap_xent_backward: clearing dW", e);
+    }
+    return ASAP_OK;
+  }
+  if (ws_bytes < plan_backward(s, 1).end || (reinterpret_cast<uintptr_t>(ws) & 255u))
+    return reject(ASAP_ERR_ARG, "asap_xent_backward: workspace too small or not at a multiple of 256 bytes");
+  const Plan p = plan_backward(s, static_cast<size_t>(ws_bytes));
+  if (p.end > ws_bytes) return reject(ASAP_ERR_ARG, "asap_xent_backward: workspace too small");
+  Device dev;
+  const asap_status st = device(&dev);
+  if (st != ASAP_OK) return st;
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  Prep q = {};
+  q.N = s.N, q.n = static_cast<int>(s.n), q.C = static_cast<int>(s.C), q.d = static_cast<int>(s.d);
+  q.X = static_cast<const uint16_t*>(X.p), q.ldx = X.ld, q.sx = s.N == 1 ? 0 : X.stride;
+  q.y = y, q.g = g, q.bf16 = bf16, q.Xc = reinterpret_cast<uint16_t*>(w + p.xc), q.rows = p.n_pad, q.ldc = p.ldc;
+  q.perm = reinterpret_cast<int*>(w + p.perm), q.nv = reinterpret_cast<int*>(w + p.nv);
+  q.scale = reinterpret_cast<float*>(w + p.scale), q.status = static_cast<int*>(ws);
+  q.dX = static_cast<uint16_t*>(const_cast<void*>(dX.p)), q.lddx = dX.ld, q.sdx = s.N == 1 ? 0 : dX.stride;
+  Gemm a = {};
+  a.N = s.N, a.n = q.n, a.C = q.C, a.d = q.d, a.bf16 = bf16;
+  a.nv = q.nv, a.scale = q.scale, a.perm = q.perm, a.y = y, a.lse = lse, a.g = g, a.status = q.status;
+  a.acc = reinterpret_cast<float*>(w + p.acc), a.acc_rows = p.n_pad, a.ld_acc = p.ld_acc, a.direct = p.direct;
+  a.tiles_d = p.tiles_d, a.splits = p.splits;
+  a.R = {reinterpret_cast<uint16_t*>(w + p.R), p.piece, p.n_pad * p.piece, 1};
+  a.dX = {q.dX, dX.ld, q.sdx, is_wide(dX, s.N)};
+  a.dW = {static_cast<uint16_t*>(const_cast<void*>(dW.p)), dW.ld, s.N == 1 ? 0 : dW.stride, is_wide(dW, s.N)};
+  CUtensorMap tx, txc, tw;
+  if (!encode(dev, &tx, bf16, X.p, s.d, s.n, s.N, X.ld, stride_of(X, s.n, s.N)) ||
+      !encode(dev, &txc, bf16, w + p.xc, s.d, p.n_pad, s.N, p.ldc, p.n_pad * p.ldc) ||
+      !encode(dev, &tw, bf16, W.p, s.d, s.C, s.N, W.ld, stride_of(W, s.C, s.N)))
+    return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
+  Launch l;
+  l.stream = stream;
+  cudaError_t e = launch_prepare(l, q);
+  for (long long v0 = 0; v0 < s.C && e == cudaSuccess; v0 += p.piece) {
+    a.v0 = static_cast<int>(v0);
+    a.width = static_cast<int>(std::min<long long>(p.piece, s.C - v0));
+    a.first = v0 == 0;
+    CUtensorMap tr;
+    if (!encode(dev, &tr, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece))
+      return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
+    a.tiles_v = (a.width + kTile - 1) / kTile;
+    e = launch_gemm<kResidual>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * a.tiles_v, tx, txc, tw, tr);
+    if (e == cudaSuccess)
+      e = launch_gemm<kGrads>(l, dev, a, static_cast<long long>(s.N) * p.tiles_d * ((dX.p ? static_cast<long long>(p.tiles_m) * p.splits : 0) + (dW.p ? a.tiles_v : 0)),
+                              tx, txc, tw, tr);
+  }
+  if (e == cudaSuccess && dX.p && !p.direct)
+    e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N), 256, 0, false),
+                           k_finish_dx, static_cast<const float*>(a.acc), p.splits, a.N, a.acc_rows, a.ld_acc, a.perm, a.nv,
+                           a.scale, a.n, a.d, a.bf16, q.dX, q.lddx, q.sdx, static_cast<const int*>(a.status));
+  return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_backward: launch failed", e);
+}
+
+}  // namespace
+
+extern "C" asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int backward_pass, uint64_t* least,
+                                           uint64_t* bytes) {
+  const Shape s = {N, n, C, d};
+  if (!sizes_ok(s)) return reject(ASAP_ERR_ARG, "asap_xent_workspace: need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256");
+  if (!least && !bytes) return reject(ASAP_ERR_ARG, "asap_xent_workspace: NULL pointer");
+  if (least) *least = backward_pass ? plan_backward(s, 1).end : plan_forward(s).end;
+  if (bytes) *bytes = backward_pass ? plan_backward(s, 0).end : plan_forward(s).end;
+  return ASAP_OK;
+}
+
+extern "C" asap_status asap_xent_forward(int N, int64_t n, int64_t C, int64_t d, int32_t dtype, const void* X, int64_t ldx,
+                                         int64_t stride_x, const void* W, int64_t ldw, int64_t stride_w, const int32_t* y,
+                                         float* loss, float* lse, void* workspace, uint64_t workspace_bytes,
+                                         void* cuda_stream) {
+  return forward({N, n, C, d}, dtype, {X, ldx, stride_x}, {W, ldw, stride_w}, y, loss, lse, workspace, workspace_bytes,
+                 static_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" asap_status asap_xent_backward(int N, int64_t n, int64_t C, int64_t d, int32_t dtype, const void* X, int64_t ldx,
+                                          int64_t stride_x, const void* W, int64_t ldw, int64_t stride_w, const int32_t* y,
+                                          const float* lse, const float* g, void* dX, int64_t lddx, int64_t stride_dx,
+                                          void* dW, int64_t lddw, int64_t stride_dw, void* workspace,
+                                          uint64_t workspace_bytes, void* cuda_stream) {
+  return backward({N, n, C, d}, dtype, {X, ldx, stride_x}, {W, ldw, stride_w}, y, lse, g, {dX, lddx, stride_dx},
+                  {dW, lddw, stride_dw}, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}

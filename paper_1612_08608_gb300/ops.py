@@ -79,6 +79,87 @@ def _workspace(workspace: Optional[torch.Tensor], size: int, device) -> torch.Te
     return workspace
 
 
+def xent_workspace(N: int, n: int, classes: int, d: int, grad: bool = False) -> tuple:
+    """(least, good) bytes of workspace of softmax_xent, or of softmax_xent_grad, for X [N, n, d] and W [N, classes, d]."""
+    least, good = C.c_uint64(), C.c_uint64()
+    _call(load_library().asap_xent_workspace(N, n, classes, d, int(grad), C.byref(least), C.byref(good)))
+    return least.value, good.value
+
+
+def _matrix(name: str, t: torch.Tensor):
+    """(pointer, ld, stride) of [rows, d] or [N, rows, d] with unit stride in a row."""
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("%s: need rows of adjacent elements" % name)
+    rows = t.shape[-2]
+    ld = t.stride(-2) if rows > 1 else max(t.stride(-2), (t.shape[-1] + 7) // 8 * 8)
+    return t.data_ptr(), ld, t.stride(0) if t.dim() == 3 else 0
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """An empty tensor of t's shape in rows of a multiple of 16 bytes."""
+    d = t.shape[-1]
+    return torch.empty((*t.shape[:-1], (d + 7) // 8 * 8), dtype=t.dtype, device=t.device)[..., :d]
+
+
+def _xent_shapes(X, W, y):
+    if X.dim() not in (2, 3) or W.dim() != X.dim() or X.shape[-1] != W.shape[-1] or X.shape[:-2] != W.shape[:-2]:
+        raise ValueError("need X [N, n, d] and W [N, C, d], or X [n, d] and W [C, d]: got %s and %s" %
+                         (tuple(X.shape), tuple(W.shape)))
+    if X.dtype != W.dtype or X.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("need X and W in bfloat16 or float16: got %s and %s" % (X.dtype, W.dtype))
+    _packed("y", y, X, torch.int32)
+    return (X.shape[0] if X.dim() == 3 else 1, X.shape[-2], W.shape[-2], X.shape[-1])
+
+
+def _packed(name: str, t: torch.Tensor, X: torch.Tensor, dtype):
+    if t.dtype != dtype or t.shape != X.shape[:-1] or not t.is_contiguous():
+        raise ValueError("%s: need contiguous %s %s" % (name, dtype, tuple(X.shape[:-1])))
+
+
+def softmax_xent(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor, loss: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> tuple:
+    """Softmax cross entropy of the logits X W^T against the class ids y, without keeping them: (loss, lse), float32 a
+    row.  X [n, d] and W [C, d], or [N, n, d] and [N, C, d] for N workers, bfloat16 or float16; y int32 [n] or
+    [N, n].  Rows with y < 0 are left out (loss and lse 0)."""
+    N, n, classes, d = _xent_shapes(X, W, y)
+    loss = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device) if loss is None else loss
+    lse = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device) if lse is None else lse
+    _packed("loss", loss, X, torch.float32)
+    _packed("lse", lse, X, torch.float32)
+    device = _one_device([X, W, y, loss, lse])
+    workspace = _workspace(workspace, 0 if workspace is not None else xent_workspace(N, n, classes, d)[1], device)
+    with torch.cuda.device(device):
+        _call(load_library().asap_xent_forward(N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
+                                               y.data_ptr(), loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+                                               workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    return loss, lse
+
+
+def softmax_xent_grad(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, g: torch.Tensor,
+                      dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, need_dX: bool = True,
+                      need_dW: bool = True, workspace: Optional[torch.Tensor] = None) -> tuple:
+    """Gradients of (g * loss).sum() for softmax_xent's loss and lse: (dX, dW) of X's type, None for one that is not
+    needed.  g: float32, a row's weight (1 / rows for a mean).  A larger workspace takes the vocabulary in fewer pieces."""
+    N, n, classes, d = _xent_shapes(X, W, y)
+    _packed("lse", lse, X, torch.float32)
+    _packed("g", g, X, torch.float32)
+    dX = None if not need_dX else _like(X) if dX is None else dX
+    dW = None if not need_dW else _like(W) if dW is None else dW
+    held = [t for t in (dX, dW) if t is not None]
+    for t, like in ((dX, X), (dW, W)):
+        if t is not None and (t.dtype != like.dtype or t.shape != like.shape):
+            raise ValueError("need dX and dW of X's and W's shapes and types")
+    device = _one_device([X, W, y, lse, g, *held])
+    workspace = _workspace(workspace, 0 if workspace is not None else xent_workspace(N, n, classes, d, True)[1], device)
+    with torch.cuda.device(device):
+        _call(load_library().asap_xent_backward(N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
+                                                y.data_ptr(), lse.data_ptr(), g.data_ptr(),
+                                                *(_matrix("dX", dX) if need_dX else (None, 0, 0)),
+                                                *(_matrix("dW", dW) if need_dW else (None, 0, 0)), workspace.data_ptr(),
+                                                workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    return dX, dW
+
+
 def clip_workspace(n_groups: int = 1) -> int:
     """Bytes of workspace of clip_grads and sgd_step."""
     size = C.c_uint64()
