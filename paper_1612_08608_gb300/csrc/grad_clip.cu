@@ -41,6 +41,7 @@ using namespace asap;
 
 constexpr int kThreads = 512;
 constexpr int kChunk = 16384;                // elements
+constexpr int kStepUnroll = 2;             // groups of eight elements of the step in flight, a thread
 constexpr int kMaxBlocks = 1024;             // slots for partial sums: this and one for each group
 constexpr int kMaxGroups = 65536;
 
@@ -303,9 +304,32 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, const Range& r, flo
   }
 }
 
+// 32 bytes at a time: two vectors.
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  uint32_t u[8];
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "l"(p));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
+}
+
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               :: "l"(p), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+                  "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+                  "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
+}
+
+template <typename E>
+__device__ __forceinline__ void load8(const E* p, float (&v)[8]) {
+  const Vec<E> x = load_vec(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = as_float(x.e[e % Vec<E>::kN]);
+}
+
 template <typename E, typename H, bool kCopy>
 __device__ __forceinline__ void step_chunk(const Tensor& t, const Range& r, float decay, float rate) {
-  constexpr int kN = 8;                             // two vectors of parameters, one of a 16-bit copy
+  constexpr int kN = 8;                             // 32 bytes of parameters
   const E* g = static_cast<const E*>(t.g);
   float* w = static_cast<float*>(t.a);
   H* c = static_cast<H*>(t.c);
@@ -319,33 +343,33 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Range& r, floa
     return;
   }
   const long long nv = (r.end - r.body) / kN;
-#pragma unroll 2
-  for (long long v = threadIdx.x; v < nv; v += kThreads) {
-    const long long i = r.body + v * kN;
-    float gv[kN];
-    if (sizeof(E) == 2) {
-      const Vec<E> x = load_vec(g + i);
+  auto step = [&](long long i, const float (&gv)[8], float (&p)[8]) {
 #pragma unroll
-      for (int e = 0; e < kN; ++e) gv[e] = as_float(x.e[e % Vec<E>::kN]);
-    } else {
+    for (int e = 0; e < kN; ++e) p[e] = fmaf(-rate, gv[e], decay * p[e]);
+    store8(w + i, p);
+    if (kCopy) {
+      Vec<H> q;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const Vec<E> x = load_vec(g + i + 4 * h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) gv[4 * h + e] = as_float(x.e[e]);
-      }
+      for (int e = 0; e < kN; ++e) q.e[e] = from_float<H>(p[e]);
+      store_vec(c + i, q);
     }
-    Vec<float> p[2] = {load_vec(w + i), load_vec(w + i + 4)};
-    Vec<H> q;
+  };
+  long long v = threadIdx.x;
+  for (; v + (kStepUnroll - 1) * kThreads < nv; v += kStepUnroll * kThreads) {
+    float gv[kStepUnroll][8], p[kStepUnroll][8];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) {
-      const float x = fmaf(-rate, gv[e], decay * p[e >> 2].e[e & 3]);
-      p[e >> 2].e[e & 3] = x;
-      q.e[e] = from_float<H>(x);
+    for (int u = 0; u < kStepUnroll; ++u) {
+      load8(g + r.body + (v + u * kThreads) * kN, gv[u]);
+      load8(w + r.body + (v + u * kThreads) * kN, p[u]);
     }
-    store_vec(w + i, p[0]);
-    store_vec(w + i + 4, p[1]);
-    if (kCopy) store_vec(c + i, q);
+#pragma unroll
+    for (int u = 0; u < kStepUnroll; ++u) step(r.body + (v + u * kThreads) * kN, gv[u], p[u]);
+  }
+  for (; v < nv; v += kThreads) {
+    float gv[8], p[8];
+    load8(g + r.body + v * kN, gv);
+    load8(w + r.body + v * kN, p);
+    step(r.body + v * kN, gv, p);
   }
   const long long tail = r.body + nv * kN, head = r.body - r.begin;
   if (threadIdx.x < head + (r.end - tail)) one(threadIdx.x < head ? r.begin + threadIdx.x : tail + (threadIdx.x - head));
@@ -558,9 +582,8 @@ asap_status run(const Call& k, const char* const* why) {
     const uintptr_t g = reinterpret_cast<uintptr_t>(t.g), w = reinterpret_cast<uintptr_t>(t.a),
                     c = reinterpret_cast<uintptr_t>(t.c);
     auto aligned = [&](uintptr_t h) {
-      if ((g + h * es) & 15u) return false;
-      if (k.mode == kClip) return ((w + h * es) & 15u) == 0;
-      return k.mode == kNormOnly || (((w + h * 4) & 15u) == 0 && (!t.c || ((c + h * 2) & 15u) == 0));
+      if (k.mode != kStep) return ((g + h * es) & 15u) == 0 && (k.mode == kNormOnly || ((w + h * es) & 15u) == 0);
+      return ((g + h * es) & (8 * es - 1)) == 0 && ((w + h * 4) & 31u) == 0 && (!t.c || ((c + h * 2) & 15u) == 0);
     };
     uintptr_t head = 0;
     while (head < 16 && !aligned(head)) ++head;

@@ -55,14 +55,15 @@ using namespace asap;
 constexpr int kTile = 256;                     // rows and columns of a cluster's tile
 constexpr int kHalf = 128;                     // of a CTA's share
 constexpr int kTileK = 64;                     // 128 bytes: one swizzle row
-constexpr int kStages = 7;
+constexpr int kStages = 6;
 constexpr uint32_t kOperandBytes = kHalf * kTileK * 2;          // 16 KB of A, and of B
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                     // a TMA load: 64 x 64 elements
+constexpr uint32_t kOutBytes = kHalf * 32 * 2;                  // a TMA store: 32 columns of 128 rows
 constexpr int kEpiWarps = 8;                                    // two per TMEM lane quarter
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 4 * kOutBytes + 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPairs = 76;                     // clusters that a GB300 holds: what a split is sized for
@@ -91,12 +92,10 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
                : "memory");
 }
 
-// Acquires at cluster scope: arrivals come from both CTAs.
 __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-      " selp.u32 %0, 1, 0, p;\n}"
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
       : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
   return ok != 0;
 }
@@ -117,8 +116,10 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
   return r;
 }
 
+// Relaxed: it says that TMEM has been read (tcgen05.wait and fence come before it), nothing of
+// memory; a release would wait for the epilogue's stores.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
 }
 
 __device__ __forceinline__ void cluster_sync() {
@@ -137,6 +138,11 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* m, uint32
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
       "[%5];"
       :: "r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ void tma_store(const CUtensorMap* m, const void* src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+               :: "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(src)) : "memory");
 }
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -170,6 +176,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
   for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+// 32 bytes at a time.
+__device__ __forceinline__ void ld_global8(const float* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "l"(p) : "memory");
+}
+
+__device__ __forceinline__ void st_global8(float* p, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               :: "l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -221,7 +239,6 @@ struct Bool {
 struct Out {
   uint16_t* p;
   long long ld, stride;
-  int wide;                 // rows lie at multiples of 32 bytes
 };
 
 struct Gemm {
@@ -243,7 +260,7 @@ struct Gemm {
   float* zy;                // logits: [N][n] of the labels, as summed here
   float* acc;               // dX: [splits][N][rows][ld_acc]
   long long acc_rows, ld_acc;
-  Out R, dX, dW;
+  Out dX, dW;
   int* status;
 };
 
@@ -352,14 +369,17 @@ struct Walk {
   }
 };
 
-// tm_r: R; tm_x, tm_xc: X as it lies, and its rows with labels together; tm_w: W.
+// tm_r: R; tm_x, tm_xc: X as it lies, and its rows with labels together; tm_w: W;
+// tm_o1: R (residual) or dW, tm_o2: dX, to store into.
 template <int M>
 __global__ void __launch_bounds__(kThreads, 1)
     k_xent(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xc,
-           const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_r, const Gemm a) {
+           const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_r,
+           const __grid_constant__ CUtensorMap tm_o1, const __grid_constant__ CUtensorMap tm_o2, const Gemm a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(base + static_cast<size_t>(kStages) * kStageBytes);   // used in the even CTA
+  unsigned char* boxes = base + static_cast<size_t>(kStages) * kStageBytes;        // two for each half of the columns
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + 4 * kOutBytes);             // [kStages], used in the even CTA
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;                                            // [2]
   uint64_t* acc_empty = acc_full + 2;                                              // [2], used in the even CTA
@@ -491,28 +511,41 @@ __global__ void __launch_bounds__(kThreads, 1)
     int n = 0, seen = -1;                                       // accumulators drained; the worker of `scale`
     float scale = 1.f, unscale = 1.f;
     float v[32];
-    // 32 columns of this thread's row as 16-bit values, the first `left` of them: whole
-    // sectors where the rows lie at multiples of 32 bytes (wide), else groups of 16.
-    auto to_memory = [&](uint16_t* o, int left, bool wide) {
-      uint32_t u[16];
+    unsigned char* box = boxes + part * 2 * kOutBytes;
+    int boxed = 0;                                              // boxes filled
+    const bool chief = lane == 0 && ((warp - 2) & 3) == 0;      // of the four warps of a half
+    auto half_sync = [&] { asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory"); };
+    // 32 columns of this CTA's 128 rows as 16-bit values, through shared memory.  (Stored from
+    // registers, 32 bytes of 32 rows at a time, dW of 64 rows went at 2.9 TB/s.)
+    auto to_box = [&](const CUtensorMap* m, int x, int y, int z, int rows) {
+      unsigned char* to = box + (boxed & 1) * kOutBytes;
+      ++boxed;
+      if (chief) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // what it held before is read
+      half_sync();
 #pragma unroll
-      for (int j = 0; j < 16; ++j) u[j] = pack16(v[2 * j], v[2 * j + 1], a.bf16);
-      if (left >= 32 && wide) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                       :: "l"(o + 16 * q), "r"(u[8 * q]), "r"(u[8 * q + 1]), "r"(u[8 * q + 2]), "r"(u[8 * q + 3]),
-                          "r"(u[8 * q + 4]), "r"(u[8 * q + 5]), "r"(u[8 * q + 6]), "r"(u[8 * q + 7]) : "memory");
-        return;
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4*>(to + r * 64 + ((q ^ ((r >> 1) & 3)) << 4)) =    // 64-byte swizzle
+            make_uint4(pack16(v[8 * q], v[8 * q + 1], a.bf16), pack16(v[8 * q + 2], v[8 * q + 3], a.bf16),
+                       pack16(v[8 * q + 4], v[8 * q + 5], a.bf16), pack16(v[8 * q + 6], v[8 * q + 7], a.bf16));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      half_sync();
+      if (chief && y < rows) {
+        tma_store(m, to, x, y, z);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
       }
+    };
+    // The first `left` of the 32 columns to this thread's own row (at a multiple of 16 bytes).
+    auto to_row = [&](uint16_t* o, int left) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        const uint32_t u[4] = {pack16(v[8 * q], v[8 * q + 1], a.bf16), pack16(v[8 * q + 2], v[8 * q + 3], a.bf16),
+                               pack16(v[8 * q + 4], v[8 * q + 5], a.bf16), pack16(v[8 * q + 6], v[8 * q + 7], a.bf16)};
         if (left >= 8 * q + 8) {
-          *reinterpret_cast<uint4*>(o + 8 * q) = make_uint4(u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]);
+          *reinterpret_cast<uint4*>(o + 8 * q) = make_uint4(u[0], u[1], u[2], u[3]);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (left > 8 * q + e) o[8 * q + e] = static_cast<uint16_t>(u[4 * q + (e >> 1)] >> (16 * (e & 1)));
+            if (left > 8 * q + e) o[8 * q + e] = static_cast<uint16_t>(u[e >> 1] >> (16 * (e & 1)));
         }
       }
     };
@@ -597,7 +630,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (mine) a.zy[wn + row] = zy;
         }
       } else if (M == kResidual) {
-        uint16_t* out = a.R.p + w.worker * a.R.stride + static_cast<long long>(row) * a.R.ld;
         for (int c = 0; c < 4; ++c) {
           const int cc = col0 + 32 * c;
           if (cc >= a.width) break;
@@ -607,15 +639,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float p = ex2(fmaf(v[j], kLog2e, off)) - (cc + j == yb ? 1.f : 0.f);
             v[j] = live && cc + j < a.width ? gs * p : 0.f;
           }
-          to_memory(out + cc, 32, true);                             // rows of R end at a multiple of 256 columns
+          to_box(&tm_o1, cc, row - r, w.worker, w.nv);
         }
       } else {
-        const bool sums = !w.dw && !a.direct;
+        // dX's rows go one by one where some are left out; so does a row's end that is no
+        // multiple of 16 bytes: a TMA store writes whole groups of them.
+        const bool sums = !w.dw && !a.direct, together = w.dw || w.nv == a.n;
         const bool stored = w.dw ? a.v0 + row < a.C : live;
-        uint16_t* out = w.dw ? a.dW.p + w.worker * a.dW.stride + (a.v0 + static_cast<long long>(row)) * a.dW.ld
-                             : a.dX.p + w.worker * a.dX.stride + static_cast<long long>(at) * a.dX.ld;
-        const bool wide = w.dw ? a.dW.wide : a.dX.wide;
-        float* acc = a.acc + ((static_cast<long long>(w.split) * a.N + w.worker) * a.acc_rows + row) * a.ld_acc;
         for (int c = 0; c < 4; ++c) {
           const int cc = col0 + 32 * c;
           if (cc >= a.d) break;
@@ -625,26 +655,30 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0.f;
           }
-          if (!stored) continue;
           if (!sums) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] *= unscale;
-            to_memory(out + cc, a.d - cc, wide);
+            if (together && (cc + 32 <= a.d || (a.d & 7) == 0)) {
+              if (w.dw) to_box(&tm_o1, cc, a.v0 + row - r, w.worker, a.C);
+              else to_box(&tm_o2, cc, row - r, w.worker, a.n);
+            } else if (stored) {
+              const Out& out = w.dw ? a.dW : a.dX;
+              to_row(out.p + w.worker * out.stride + (w.dw ? a.v0 + static_cast<long long>(row) : at) * out.ld + cc, a.d - cc);
+            }
             continue;
           }
-          float4* o = reinterpret_cast<float4*>(acc + cc);
+          if (!stored) continue;
+          float* o = a.acc + ((static_cast<long long>(w.split) * a.N + w.worker) * a.acc_rows + row) * a.ld_acc + cc;
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            if (cc + 4 * u >= a.ld_acc) break;
-            float4 x = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+          for (int q = 0; q < 4; ++q) {
+            if (cc + 8 * q >= a.ld_acc) break;
             if (!a.first) {
-              const float4 p = o[u];
-              x.x += p.x;
-              x.y += p.y;
-              x.z += p.z;
-              x.w += p.w;
+              float p[8];
+              ld_global8(o + 8 * q, p);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[8 * q + e] += p[e];
             }
-            o[u] = x;
+            st_global8(o + 8 * q, v + 8 * q);
           }
         }
       }
@@ -655,6 +689,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++n;
       }
     }
+    // The boxes are given back with no copy in flight, and what they held is in memory.
+    if (chief) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
   }
   tc_fence_before();
   __syncthreads();
@@ -936,16 +973,17 @@ asap_status device(Device* out) {
   return ASAP_OK;
 }
 
-// [N][rows][inner] of 16-bit elements; boxes of 64 x 64, 128-byte swizzle.
+// [N][rows][inner] of 16-bit elements; boxes of 64 x 64 in 128-byte swizzle to load, of 32 x
+// 128 in 64-byte swizzle to store.
 bool encode(const Device& dev, CUtensorMap* m, bool bf16, const void* base, long long inner, long long rows, long long N,
-            long long ld, long long stride) {
+            long long ld, long long stride, bool store = false) {
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(N)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(stride) * 2};
-  const cuuint32_t box[3] = {64, 64, 1};
+  const cuuint32_t box[3] = {store ? 32u : 64u, store ? static_cast<cuuint32_t>(kHalf) : 64u, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return dev.encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                     const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    store ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -986,7 +1024,7 @@ Plan plan_common(const Shape& s) {
   Plan p = {};
   p.n_pad = up(s.n, kTile);
   p.ldc = up(s.d, 8);
-  p.ld_acc = up(s.d, 4);
+  p.ld_acc = up(s.d, 8);
   p.tiles_m = static_cast<int>(p.n_pad / kTile);
   p.tiles_v = static_cast<int>(up(s.C, kTile) / kTile);
   p.tiles_d = static_cast<int>(up(s.d, kTile) / kTile);
@@ -1053,10 +1091,6 @@ bool matrix_ok(const Matrix& m, long long rows, long long d, int N) {
 
 long long stride_of(const Matrix& m, long long rows, int N) { return N == 1 ? std::max(8LL, rows * m.ld) : m.stride; }
 
-bool is_wide(const Matrix& m, int N) {
-  return ((reinterpret_cast<uintptr_t>(m.p) | static_cast<uintptr_t>(m.ld * 2) | static_cast<uintptr_t>(N == 1 ? 0 : m.stride * 2)) & 31u) == 0;
-}
-
 // The bytes from the first to behind the last element.
 struct Extent {
   uintptr_t begin, end;
@@ -1115,9 +1149,10 @@ struct Launch {
 
 template <int M>
 cudaError_t launch_gemm(Launch& l, const Device& dev, const Gemm& a, long long tiles, const CUtensorMap& tx,
-                        const CUtensorMap& txc, const CUtensorMap& tw, const CUtensorMap& tr) {
+                        const CUtensorMap& txc, const CUtensorMap& tw, const CUtensorMap& tr, const CUtensorMap& to1,
+                        const CUtensorMap& to2) {
   const int clusters = static_cast<int>(std::min<long long>(tiles, dev.clusters));
-  return cudaLaunchKernelEx(l.at(dim3(2 * clusters), kThreads, kSmemBytes, true), k_xent<M>, tx, txc, tw, tr, a);
+  return cudaLaunchKernelEx(l.at(dim3(2 * clusters), kThreads, kSmemBytes, true), k_xent<M>, tx, txc, tw, tr, to1, to2, a);
 }
 
 cudaError_t launch_prepare(Launch& l, Prep q) {
@@ -1173,7 +1208,7 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   Launch l;
   l.stream = stream;
   cudaError_t e = launch_prepare(l, q);
-  if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw);
+  if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw, tw, tw);
   if (e == cudaSuccess)
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
                            static_cast<const float2*>(a.part), 2 * p.tiles_v, static_cast<const float*>(q.zy), static_cast<const float*>(a.zy), a.perm, a.nv,
@@ -1225,13 +1260,14 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
   a.nv = q.nv, a.scale = q.scale, a.perm = q.perm, a.y = y, a.lse = lse, a.g = g, a.status = q.status;
   a.acc = reinterpret_cast<float*>(w + p.acc), a.acc_rows = p.n_pad, a.ld_acc = p.ld_acc, a.direct = p.direct;
   a.tiles_d = p.tiles_d, a.splits = p.splits;
-  a.R = {reinterpret_cast<uint16_t*>(w + p.R), p.piece, p.n_pad * p.piece, 1};
-  a.dX = {q.dX, dX.ld, q.sdx, is_wide(dX, s.N)};
-  a.dW = {static_cast<uint16_t*>(const_cast<void*>(dW.p)), dW.ld, s.N == 1 ? 0 : dW.stride, is_wide(dW, s.N)};
-  CUtensorMap tx, txc, tw;
+  a.dX = {q.dX, dX.ld, q.sdx};
+  a.dW = {static_cast<uint16_t*>(const_cast<void*>(dW.p)), dW.ld, s.N == 1 ? 0 : dW.stride};
+  CUtensorMap tx, txc, tw, tdx, tdw;
   if (!encode(dev, &tx, bf16, X.p, s.d, s.n, s.N, X.ld, stride_of(X, s.n, s.N)) ||
       !encode(dev, &txc, bf16, w + p.xc, s.d, p.n_pad, s.N, p.ldc, p.n_pad * p.ldc) ||
-      !encode(dev, &tw, bf16, W.p, s.d, s.C, s.N, W.ld, stride_of(W, s.C, s.N)))
+      !encode(dev, &tw, bf16, W.p, s.d, s.C, s.N, W.ld, stride_of(W, s.C, s.N)) ||
+      (dX.p && !encode(dev, &tdx, bf16, dX.p, s.d, s.n, s.N, dX.ld, stride_of(dX, s.n, s.N), true)) ||
+      (dW.p && !encode(dev, &tdw, bf16, dW.p, s.d, s.C, s.N, dW.ld, stride_of(dW, s.C, s.N), true)))
     return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
   Launch l;
   l.stream = stream;
@@ -1240,14 +1276,15 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
     a.v0 = static_cast<int>(v0);
     a.width = static_cast<int>(std::min<long long>(p.piece, s.C - v0));
     a.first = v0 == 0;
-    CUtensorMap tr;
-    if (!encode(dev, &tr, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece))
+    CUtensorMap tr, tro;
+    if (!encode(dev, &tr, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece) ||
+        !encode(dev, &tro, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece, true))
       return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
     a.tiles_v = (a.width + kTile - 1) / kTile;
-    e = launch_gemm<kResidual>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * a.tiles_v, tx, txc, tw, tr);
+    e = launch_gemm<kResidual>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * a.tiles_v, tx, txc, tw, tr, tro, tro);
     if (e == cudaSuccess)
       e = launch_gemm<kGrads>(l, dev, a, static_cast<long long>(s.N) * p.tiles_d * ((dX.p ? static_cast<long long>(p.tiles_m) * p.splits : 0) + (dW.p ? a.tiles_v : 0)),
-                              tx, txc, tw, tr);
+                              tx, txc, tw, tr, dW.p ? tdw : tr, dX.p ? tdx : tr);
   }
   if (e == cudaSuccess && dX.p && !p.direct)
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N), 256, 0, false),

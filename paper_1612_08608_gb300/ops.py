@@ -6,6 +6,7 @@ allocator.  Nothing here records autograd history."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Optional, Sequence
 
 import torch
@@ -30,6 +31,18 @@ def _one_device(tensors) -> torch.device:
     if device.type != "cuda":
         raise ValueError("need CUDA tensors, got %s" % device)
     return device
+
+
+def _launch(device: torch.device, fn, *args):
+    """fn(*args, stream) with `device` current, on its current stream."""
+    index = device.index
+    # the handle alone: a torch.cuda.Stream object takes as long to make as a kernel launch
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
+        _call(fn(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            _call(fn(*args, stream))
 
 
 def _pointers(tensors):
@@ -57,6 +70,8 @@ def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
             raise ValueError("%d groups for %d gradients" % (len(groups), T))
         if n_groups is None:
             n_groups = max(groups) + 1
+        if min(groups) < 0 or max(groups) >= n_groups:
+            raise ValueError("groups: need numbers from 0 to %d" % (n_groups - 1))
         groups = (C.c_int32 * T)(*groups)
     elif n_groups is None:
         n_groups = 1
@@ -64,9 +79,7 @@ def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
         norms = torch.empty(n_groups, dtype=torch.float32, device=device)
     elif norms.dtype != torch.float32 or norms.shape != (n_groups,) or not norms.is_contiguous() or norms.device != device:
         raise ValueError("norms: need %d contiguous float32 on %s" % (n_groups, device))
-    size = C.c_uint64()
-    _call(load_library().asap_clip_workspace(n_groups, C.byref(size)))
-    workspace = _workspace(workspace, size.value, device)
+    workspace = _workspace(workspace, 0 if workspace is not None else clip_workspace(n_groups), device)
     arrays = (_pointers(grads), (C.c_int64 * T)(*[g.numel() for g in grads]), (C.c_int32 * T)(*dtypes))
     return device, arrays, groups, n_groups, norms, workspace
 
@@ -79,6 +92,7 @@ def _workspace(workspace: Optional[torch.Tensor], size: int, device) -> torch.Te
     return workspace
 
 
+@functools.lru_cache(maxsize=256)
 def xent_workspace(N: int, n: int, classes: int, d: int, grad: bool = False) -> tuple:
     """(least, good) bytes of workspace of softmax_xent, or of softmax_xent_grad, for X [N, n, d] and W [N, classes, d]."""
     least, good = C.c_uint64(), C.c_uint64()
@@ -128,10 +142,8 @@ def softmax_xent(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor, loss: Option
     _packed("lse", lse, X, torch.float32)
     device = _one_device([X, W, y, loss, lse])
     workspace = _workspace(workspace, 0 if workspace is not None else xent_workspace(N, n, classes, d)[1], device)
-    with torch.cuda.device(device):
-        _call(load_library().asap_xent_forward(N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
-                                               y.data_ptr(), loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
-                                               workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    _launch(device, load_library().asap_xent_forward, N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
+            y.data_ptr(), loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel())
     return loss, lse
 
 
@@ -151,15 +163,13 @@ def softmax_xent_grad(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor, lse: to
             raise ValueError("need dX and dW of X's and W's shapes and types")
     device = _one_device([X, W, y, lse, g, *held])
     workspace = _workspace(workspace, 0 if workspace is not None else xent_workspace(N, n, classes, d, True)[1], device)
-    with torch.cuda.device(device):
-        _call(load_library().asap_xent_backward(N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
-                                                y.data_ptr(), lse.data_ptr(), g.data_ptr(),
-                                                *(_matrix("dX", dX) if need_dX else (None, 0, 0)),
-                                                *(_matrix("dW", dW) if need_dW else (None, 0, 0)), workspace.data_ptr(),
-                                                workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    _launch(device, load_library().asap_xent_backward, N, n, classes, d, DTYPE[X.dtype], *_matrix("X", X), *_matrix("W", W),
+            y.data_ptr(), lse.data_ptr(), g.data_ptr(), *(_matrix("dX", dX) if need_dX else (None, 0, 0)),
+            *(_matrix("dW", dW) if need_dW else (None, 0, 0)), workspace.data_ptr(), workspace.numel())
     return dX, dW
 
 
+@functools.lru_cache(maxsize=64)
 def clip_workspace(n_groups: int = 1) -> int:
     """Bytes of workspace of clip_grads and sgd_step."""
     size = C.c_uint64()
@@ -185,10 +195,8 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
     device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
                                                                                        workspace, out or ())
     dst = None if only else ptrs if out is None else _pointers(out)
-    with torch.cuda.device(device):
-        _call(load_library().asap_clip_grads(len(grads), ptrs, dst, numel, dtypes, groups, n_groups, max_norm,
-                                             norms.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                             torch.cuda.current_stream().cuda_stream))
+    _launch(device, load_library().asap_clip_grads, len(grads), ptrs, dst, numel, dtypes, groups, n_groups, max_norm,
+            norms.data_ptr(), workspace.data_ptr(), workspace.numel())
     return norms
 
 
@@ -216,8 +224,6 @@ def sgd_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: 
     if copies is not None:
         cptr = _pointers(copies)
         ctype = (C.c_int32 * len(copies))(*[0 if c is None else DTYPE[c.dtype] for c in copies])
-    with torch.cuda.device(device):
-        _call(load_library().asap_sgd_clipped(len(grads), _pointers(params), cptr, ctype, ptrs, numel, dtypes, groups,
-                                              n_groups, max_norm, lr, l2, norms.data_ptr(), workspace.data_ptr(),
-                                              workspace.numel(), torch.cuda.current_stream().cuda_stream))
+    _launch(device, load_library().asap_sgd_clipped, len(grads), _pointers(params), cptr, ctype, ptrs, numel, dtypes, groups,
+            n_groups, max_norm, lr, l2, norms.data_ptr(), workspace.data_ptr(), workspace.numel())
     return norms
