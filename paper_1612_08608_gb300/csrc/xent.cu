@@ -11,9 +11,9 @@
 // each CTA keeps 128 rows of the accumulator in its TMEM, and brings 128 rows of A
 // and 128 of B; a tile costs each SM a third less shared-memory reading than one of
 // 128 x 256 of its own).  Per CTA: one warp issues TMA loads into a ring of stages, one
-// (of the even CTA) the MMAs, and eight drain the other of two accumulators:
-//   logits    A = X, B = W (both K-major); a row's running maximum and sum of
-//             exponentials over 128 columns go to a table, which k_finish_loss joins.
+// (of the even CTA) the MMAs, and sixteen drain the other of two accumulators:
+//   logits    A = X, B = W (both K-major); a row's maximum and sum of exponentials
+//             over a tile go to a table, which k_finish_loss joins.
 //             No logit is written.
 //   residual  the same product again for one piece of the vocabulary, with R as the
 //             epilogue, 16-bit, in the workspace
@@ -24,7 +24,7 @@
 //
 // Rows without a label cost nothing: k_prepare lists the others, and copies X's
 // rows together if any is left out (so that what stands in the others, NaN even,
-// meets no product).  It also takes the logits of the labels, in fp32 arithmetic: the
+// meets no product).  The logits of the labels are taken again, in fp32 arithmetic: the
 // tensor cores' sums are cut off after each step, which shows in the loss (d = 4096,
 // logits of 12: 3e-6 of it); k_finish_loss puts the label's term in lse right by it.  R is fp16 for fp16 operands (an MMA's have one type): it is
 // scaled by a power of two that brings the largest |g| near the top of the range.
@@ -60,10 +60,12 @@ constexpr uint32_t kOperandBytes = kHalf * kTileK * 2;          // 16 KB of A, a
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                     // a TMA load: 64 x 64 elements
 constexpr uint32_t kOutBytes = kHalf * 32 * 2;                  // a TMA store: 32 columns of 128 rows
-constexpr int kEpiWarps = 8;                                    // two per TMEM lane quarter
+constexpr int kEpiWarps = 16;                                   // four per TMEM lane quarter
+constexpr int kParts = kEpiWarps / 4;                           // parts of a tile's columns, four warps each
+constexpr int kPartCols = kTile / kParts;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 4 * kOutBytes + 256;
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + kParts * kOutBytes + 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPairs = 76;                     // clusters that a GB300 holds: what a split is sized for
@@ -224,6 +226,14 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
   return u;
 }
 
+// (m, s): a maximum, and the sum of exponentials less it.
+__device__ __forceinline__ void join(float& m, float& s, float pm, float ps) {
+  const float t = fmaxf(m, pm);
+  if (t > -INFINITY) s = s * ex2((m - t) * kLog2e) + ps * ex2((pm - t) * kLog2e);
+  else s += ps;                                                // 0, or NaN
+  m = t;
+}
+
 __device__ __forceinline__ float2 unpack16(uint32_t u, bool bf16) {
   if (bf16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
   return __half22float2(*reinterpret_cast<const __half2*>(&u));
@@ -233,6 +243,24 @@ template <bool V>
 struct Bool {
   static constexpr bool value = V;
 };
+
+// The dot product of two rows of d 16-bit elements (16-byte aligned) by a warp, in every lane.
+__device__ __forceinline__ float dot16(const uint16_t* x, const uint16_t* w, int d, bool bf16, int lane) {
+  float z = 0.f;
+#pragma unroll 4
+  for (int v = lane; v < d / 8; v += 32) {
+    const uint4 p = reinterpret_cast<const uint4*>(x)[v], q = reinterpret_cast<const uint4*>(w)[v];
+    const float2 x0 = unpack16(p.x, bf16), x1 = unpack16(p.y, bf16), x2 = unpack16(p.z, bf16), x3 = unpack16(p.w, bf16);
+    const float2 w0 = unpack16(q.x, bf16), w1 = unpack16(q.y, bf16), w2 = unpack16(q.z, bf16), w3 = unpack16(q.w, bf16);
+    z += (fmaf(x0.x, w0.x, x0.y * w0.y) + fmaf(x1.x, w1.x, x1.y * w1.y)) +
+         (fmaf(x2.x, w2.x, x2.y * w2.y) + fmaf(x3.x, w3.x, x3.y * w3.y));
+  }
+  const int c = d / 8 * 8 + lane;
+  if (c < d) z = fmaf(unpack16(x[c], bf16).x, unpack16(w[c], bf16).x, z);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  return z;
+}
 
 // ---- arguments ------------------------------------------------------------------
 // A matrix of results: [N] of rows of 16-bit elements.
@@ -256,8 +284,10 @@ struct Gemm {
   const int* y;             // [N][n]
   const float* lse;         // [N][n]
   const float* g;           // [N][n]
-  float2* part;             // logits: [N][n][2 tiles_v]
-  float* zy;                // logits: [N][n] of the labels, as summed here
+  float2* part;             // logits: [N][n][tiles_v]
+  float* zy;                // logits: [2][N][n] of the labels, exact and as summed here
+  const uint16_t *X, *W;    // logits: for the exact ones
+  long long ldx, sx, ldw, sw;
   float* acc;               // dX: [splits][N][rows][ld_acc]
   long long acc_rows, ld_acc;
   Out dX, dW;
@@ -378,8 +408,8 @@ __global__ void __launch_bounds__(kThreads, 1)
            const __grid_constant__ CUtensorMap tm_o1, const __grid_constant__ CUtensorMap tm_o2, const Gemm a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  unsigned char* boxes = base + static_cast<size_t>(kStages) * kStageBytes;        // two for each half of the columns
-  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + 4 * kOutBytes);             // [kStages], used in the even CTA
+  unsigned char* boxes = base + static_cast<size_t>(kStages) * kStageBytes;        // one for each part; logits: the parts' sums
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + kParts * kOutBytes);             // [kStages], used in the even CTA
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;                                            // [2]
   uint64_t* acc_empty = acc_full + 2;                                              // [2], used in the even CTA
@@ -505,32 +535,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else {
-    const int quarter = warp & 3, part = (warp - 2) >> 2;       // TMEM lanes; columns 128 part .. +127
+    const int quarter = warp & 3, part = (warp - 2) >> 2;       // TMEM lanes; columns kPartCols part ..
     const int r = quarter * 32 + lane;                          // row of this CTA's share
     const uint32_t release[2] = {cluster_addr(acc_empty, 0), cluster_addr(acc_empty + 1, 0)};
     int n = 0, seen = -1;                                       // accumulators drained; the worker of `scale`
     float scale = 1.f, unscale = 1.f;
     float v[32];
-    unsigned char* box = boxes + part * 2 * kOutBytes;
-    int boxed = 0;                                              // boxes filled
-    const bool chief = lane == 0 && ((warp - 2) & 3) == 0;      // of the four warps of a half
-    auto half_sync = [&] { asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory"); };
+    unsigned char* box = boxes + part * kOutBytes;
+    const bool chief = lane == 0 && ((warp - 2) & 3) == 0;      // of the four warps of a part
+    auto part_sync = [&] { asm volatile("bar.sync %0, 128;" :: "r"(2 + part) : "memory"); };
     // 32 columns of this CTA's 128 rows as 16-bit values, through shared memory.  (Stored from
     // registers, 32 bytes of 32 rows at a time, dW of 64 rows went at 2.9 TB/s.)
     auto to_box = [&](const CUtensorMap* m, int x, int y, int z, int rows) {
-      unsigned char* to = box + (boxed & 1) * kOutBytes;
-      ++boxed;
-      if (chief) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // what it held before is read
-      half_sync();
+      if (chief) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // what it held before is read
+      part_sync();
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<uint4*>(to + r * 64 + ((q ^ ((r >> 1) & 3)) << 4)) =    // 64-byte swizzle
+        *reinterpret_cast<uint4*>(box + r * 64 + ((q ^ ((r >> 1) & 3)) << 4)) =    // 64-byte swizzle
             make_uint4(pack16(v[8 * q], v[8 * q + 1], a.bf16), pack16(v[8 * q + 2], v[8 * q + 3], a.bf16),
                        pack16(v[8 * q + 4], v[8 * q + 5], a.bf16), pack16(v[8 * q + 6], v[8 * q + 7], a.bf16));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      half_sync();
+      part_sync();
       if (chief && y < rows) {
-        tma_store(m, to, x, y, z);
+        tma_store(m, box, x, y, z);
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
       }
     };
@@ -549,9 +576,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     };
+    auto release_acc = [&] {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(release[n & 1]);
+    };
     while (w.next()) {
       const int row = w.m * kTile + static_cast<int>(rank) * kHalf + r;   // of the tile's matrix
-      const int col0 = w.nn * kTile + part * kHalf;                       // this thread's first column
+      const int col0 = w.nn * kTile + part * kPartCols;                   // this thread's first column
       const long long wn = static_cast<long long>(w.worker) * a.n;
       const bool live = !w.dw && row < w.nv;
       if (M != kLogits && w.worker != seen) {
@@ -568,14 +600,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         off = -a.lse[wn + at] * kLog2e;
         gs = a.g[wn + at] * scale;
       }
+      if (M == kLogits) {
+        // The logits of the labels in the tile, in fp32 arithmetic, while its products are
+        // summed: they read the same rows.  The warps of a quarter take every fourth row.
+        unsigned mine = __ballot_sync(0xffffffffu, yb >= w.nn * kTile && yb < (w.nn + 1) * kTile) & (0x11111111u << part);
+        while (mine) {
+          const int q = __ffs(mine) - 1;
+          mine &= mine - 1;
+          const long long xr = __shfl_sync(0xffffffffu, at, q), wr = __shfl_sync(0xffffffffu, yb, q);
+          const float z = dot16(a.X + w.worker * a.sx + xr * a.ldx, a.W + w.worker * a.sw + wr * a.ldw, a.d, a.bf16, lane);
+          if (lane == 0) a.zy[wn + row + q] = z;
+        }
+      }
       const int ab = n & 1;
       if (w.kt > 0) {
-        // All threads of a half go on or give up together: they meet at its barrier.
+        // All go on or give up together: they meet at barriers.
         const bool ok = mbar_wait(acc_full + ab, static_cast<uint32_t>((n >> 1) & 1));
         uint32_t bad;
         asm volatile(
-            "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
-            : "=r"(bad) : "r"(static_cast<uint32_t>(!ok)), "r"(1 + part) : "memory");
+            "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+            : "=r"(bad) : "r"(static_cast<uint32_t>(!ok)), "n"(kEpiWarps * 32) : "memory");
         if (bad) {
           fail(a.status);
           if (M == kGrads && lane == 0 && warp == 2 && rank == 0) {
@@ -588,11 +632,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
       }
       const uint32_t trow = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(ab) * kTile +
-                            static_cast<uint32_t>(part) * kHalf;
+                            static_cast<uint32_t>(part) * kPartCols;
       if (M == kLogits) {
         float m = -INFINITY, s = 0.f, zy = 0.f;
         bool mine = false;
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kPartCols / 32; ++c) {
           const int cc = col0 + 32 * c;
           if (cc >= a.C) break;
           tmem_ld32(trow + 32 * c, v);
@@ -625,12 +669,22 @@ __global__ void __launch_bounds__(kThreads, 1)
           s += (s0 + s1) + (s2 + s3);
           m = cm;
         }
-        if (live) {
-          a.part[(wn + row) * (2 * a.tiles_v) + 2 * w.nn + part] = make_float2(m, s);
-          if (mine) a.zy[wn + row] = zy;
+        if (mine) a.zy[static_cast<long long>(a.N) * a.n + wn + row] = zy;
+        // The parts' sums meet in shared memory (that of a tile and the next in turn: who is
+        // still joining one has yet to come to the other's barrier).
+        float2* sums = reinterpret_cast<float2*>(boxes) + ab * kParts * kHalf;
+        if (part) sums[part * kHalf + r] = make_float2(m, s);
+        asm volatile("bar.sync 2, %0;" :: "n"(kEpiWarps * 32) : "memory");
+        if (part == 0 && live) {
+#pragma unroll
+          for (int q = 1; q < kParts; ++q) {
+            const float2 p = sums[q * kHalf + r];
+            join(m, s, p.x, p.y);
+          }
+          a.part[(wn + row) * a.tiles_v + w.nn] = make_float2(m, s);
         }
       } else if (M == kResidual) {
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kPartCols / 32; ++c) {
           const int cc = col0 + 32 * c;
           if (cc >= a.width) break;
           tmem_ld32(trow + 32 * c, v);
@@ -646,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // multiple of 16 bytes: a TMA store writes whole groups of them.
         const bool sums = !w.dw && !a.direct, together = w.dw || w.nv == a.n;
         const bool stored = w.dw ? a.v0 + row < a.C : live;
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kPartCols / 32; ++c) {
           const int cc = col0 + 32 * c;
           if (cc >= a.d) break;
           if (w.kt > 0) {
@@ -683,9 +737,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (w.kt > 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_at(release[ab]);
+        release_acc();
         ++n;
       }
     }
@@ -702,15 +754,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---- before: the rows with a label ---------------------------------------------------
 constexpr int kPrepThreads = 256;
-constexpr int kPrepBlocks = 512;            // per worker, at most
+constexpr int kPrepBlocks = 1024;           // about, of all workers
 
 struct Prep {
   int N, n, C, d, bf16, per_block;
   const uint16_t* X;
   long long ldx, sx;
-  const uint16_t* W;        // forward: for the logits of the labels
-  long long ldw, sw;
-  float* zy;                // [N][n], by place in perm
   const int* y;
   const float* g;           // backward: the largest |g| sets the scale of R
   uint16_t* Xc;             // [N][rows][ldc]
@@ -788,7 +837,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
     }
     for (int q = warp; q < 32; q += kPrepThreads / 32) {
       if (r0 + q >= end) break;
-      const int label = __shfl_sync(0xffffffffu, yr, q), at = first + __shfl_sync(0xffffffffu, place, q);
+      const int at = first + __shfl_sync(0xffffffffu, place, q);
       if (!((rows_in >> q) & 1u)) {
         if (a.dX) {
           uint16_t* dst = a.dX + worker * a.sdx + (r0 + q) * a.lddx;
@@ -801,28 +850,10 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
       const uint16_t* x = a.X + worker * a.sx + (r0 + q) * a.ldx;
       if (nv < a.n) {
         uint16_t* dst = a.Xc + (worker * a.rows + at) * a.ldc;
+#pragma unroll 4
         for (int v = lane; v < a.d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = reinterpret_cast<const uint4*>(x)[v];
         const int c = a.d / 8 * 8 + lane;
         if (c < a.d) dst[c] = x[c];
-      }
-      if (a.zy) {
-        const uint16_t* w = a.W + worker * a.sw + label * a.ldw;
-        float z = 0.f;
-#pragma unroll 4
-        for (int v = lane; v < a.d / 8; v += 32) {
-          const uint4 p = reinterpret_cast<const uint4*>(x)[v], r = reinterpret_cast<const uint4*>(w)[v];
-          const float2 x0 = unpack16(p.x, a.bf16), x1 = unpack16(p.y, a.bf16), x2 = unpack16(p.z, a.bf16),
-                       x3 = unpack16(p.w, a.bf16);
-          const float2 w0 = unpack16(r.x, a.bf16), w1 = unpack16(r.y, a.bf16), w2 = unpack16(r.z, a.bf16),
-                       w3 = unpack16(r.w, a.bf16);
-          z += (fmaf(x0.x, w0.x, x0.y * w0.y) + fmaf(x1.x, w1.x, x1.y * w1.y)) +
-               (fmaf(x2.x, w2.x, x2.y * w2.y) + fmaf(x3.x, w3.x, x3.y * w3.y));
-        }
-        const int c = a.d / 8 * 8 + lane;
-        if (c < a.d) z = fmaf(unpack16(x[c], a.bf16).x, unpack16(w[c], a.bf16).x, z);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0) a.zy[wn + at] = z;
       }
     }
     first += __popc(rows_in);
@@ -848,18 +879,12 @@ __global__ void __launch_bounds__(kLossWarps * 32)
   if (row >= nv[worker]) return;
   part += (wn + row) * slots;
   float m = -INFINITY, s = 0.f;
-  auto join = [&](float pm, float ps) {
-    const float t = fmaxf(m, pm);
-    if (t > -INFINITY) s = s * ex2((m - t) * kLog2e) + ps * ex2((pm - t) * kLog2e);
-    else s += ps;                                               // 0, or NaN
-    m = t;
-  };
 #pragma unroll 4
-  for (int q = lane; q < slots; q += 32) join(part[q].x, part[q].y);
+  for (int q = lane; q < slots; q += 32) join(m, s, part[q].x, part[q].y);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const float pm = __shfl_xor_sync(0xffffffffu, m, o), ps = __shfl_xor_sync(0xffffffffu, s, o);
-    join(pm, ps);
+    join(m, s, pm, ps);
   }
   if (lane != 0) return;
   const bool dead = *static_cast<const volatile int*>(status) != 0;
@@ -1039,7 +1064,7 @@ Plan plan_common(const Shape& s) {
 
 Plan plan_forward(const Shape& s) {
   Plan p = plan_common(s);
-  p.part = take(p.end, 8 * static_cast<size_t>(s.N) * 2 * p.tiles_v * s.n);
+  p.part = take(p.end, 8 * static_cast<size_t>(s.N) * p.tiles_v * s.n);
   p.zy = take(p.end, 8 * static_cast<size_t>(s.N) * s.n);
   return p;
 }
@@ -1157,8 +1182,7 @@ cudaError_t launch_gemm(Launch& l, const Device& dev, const Gemm& a, long long t
 
 cudaError_t launch_prepare(Launch& l, Prep q) {
   // a row for each warp while there are few
-  const int rows = (q.n + kPrepBlocks - 1) / kPrepBlocks;
-  q.per_block = rows <= 8 ? 8 : static_cast<int>(up(rows, 32));
+  q.per_block = static_cast<int>(up((static_cast<long long>(q.N) * q.n + kPrepBlocks - 1) / kPrepBlocks, 8));
   return cudaLaunchKernelEx(l.at(dim3((q.n + q.per_block - 1) / q.per_block, q.N), kPrepThreads, 0, false), k_prepare, q);
 }
 
@@ -1195,8 +1219,7 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   Prep q = {};
   q.N = s.N, q.n = static_cast<int>(s.n), q.C = static_cast<int>(s.C), q.d = static_cast<int>(s.d);
   q.X = static_cast<const uint16_t*>(X.p), q.ldx = X.ld, q.sx = s.N == 1 ? 0 : X.stride;
-  q.W = static_cast<const uint16_t*>(W.p), q.ldw = W.ld, q.sw = s.N == 1 ? 0 : W.stride;
-  q.zy = reinterpret_cast<float*>(w + p.zy), q.bf16 = bf16;
+  q.bf16 = bf16;
   q.y = y, q.Xc = reinterpret_cast<uint16_t*>(w + p.xc), q.rows = p.n_pad, q.ldc = p.ldc;
   q.perm = reinterpret_cast<int*>(w + p.perm), q.nv = reinterpret_cast<int*>(w + p.nv);
   q.scale = reinterpret_cast<float*>(w + p.scale), q.loss = loss, q.lse = lse, q.status = static_cast<int*>(ws);
@@ -1204,14 +1227,16 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   a.N = s.N, a.n = q.n, a.C = q.C, a.d = q.d, a.bf16 = bf16, a.width = q.C;
   a.tiles_v = p.tiles_v, a.tiles_d = p.tiles_d, a.splits = 1;
   a.nv = q.nv, a.scale = q.scale, a.perm = q.perm, a.y = y;
-  a.part = reinterpret_cast<float2*>(w + p.part), a.zy = q.zy + s.N * s.n, a.status = q.status;
+  a.X = q.X, a.ldx = X.ld, a.sx = q.sx;
+  a.W = static_cast<const uint16_t*>(W.p), a.ldw = W.ld, a.sw = s.N == 1 ? 0 : W.stride;
+  a.part = reinterpret_cast<float2*>(w + p.part), a.zy = reinterpret_cast<float*>(w + p.zy), a.status = q.status;
   Launch l;
   l.stream = stream;
   cudaError_t e = launch_prepare(l, q);
   if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw, tw, tw);
   if (e == cudaSuccess)
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
-                           static_cast<const float2*>(a.part), 2 * p.tiles_v, static_cast<const float*>(q.zy), static_cast<const float*>(a.zy), a.perm, a.nv,
+                           static_cast<const float2*>(a.part), p.tiles_v, static_cast<const float*>(a.zy), static_cast<const float*>(a.zy + s.N * s.n), a.perm, a.nv,
                            a.n, loss, lse, static_cast<const int*>(a.status));
   return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
 }
