@@ -39,7 +39,8 @@ namespace {
 
 using namespace asap;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
+constexpr int kBlocksPerSm = 6;
 constexpr int kChunk = 16384;                // elements
 constexpr int kStepUnroll = 2;             // groups of eight elements of the step in flight, a thread
 constexpr int kMaxBlocks = 1024;             // slots for partial sums: this and one for each group
@@ -219,7 +220,7 @@ __device__ __forceinline__ double chunk_squares(const E* g, const Range& r, Pair
 }
 
 template <int T>
-__global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant__ Args<T> a) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_grad_squares(const __grid_constant__ Args<T> a) {
   __shared__ double red[kThreads / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int b = a.first_block + blockIdx.x;
@@ -385,7 +386,7 @@ __device__ __forceinline__ void step_any(const Tensor& t, const Range& r, float 
 enum Mode { kNormOnly, kClip, kStep };
 
 template <int T, int M>
-__global__ void __launch_bounds__(kThreads) k_grad_apply(const __grid_constant__ Args<T> a) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_grad_apply(const __grid_constant__ Args<T> a) {
   __shared__ double red[kThreads / 32];
   const int b = a.first_block + blockIdx.x;
   const int begin = max(a.chunk_begin, b * a.per);
@@ -620,7 +621,7 @@ asap_status run(const Call& k, const char* const* why) {
     set_thread_error("no usable current device");
     return ASAP_ERR_CUDA;
   }
-  const int blocks = std::min(kMaxBlocks, 3 * sms);
+  const int blocks = std::min(kMaxBlocks, kBlocksPerSm * sms);
   const int per = static_cast<int>((chunks + blocks - 1) / blocks);
   const cudaError_t e = tensors.size() <= kSmallTable ? launch<kSmallTable>(k, tensors, static_cast<int>(chunks), per)
                                                       : launch<kLargeTable>(k, tensors, static_cast<int>(chunks), per);

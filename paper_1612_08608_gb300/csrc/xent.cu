@@ -866,17 +866,155 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
     }
 }
 
+// ---- few rows: the loss alone ------------------------------------------------------------
+// One to kFewRows rows (single tokens that are scored) meet the whole head: bound by W's bytes.
+// No tensor core: a warp reads kFewCols rows of W at a time, every lane 16 bytes of each, and
+// multiplies them with X's rows from shared memory in fp32, two products an instruction.
+// Each block leaves a maximum and a sum for each row; nothing has to come before.
+constexpr int kFewRows = 4;
+constexpr int kFewCols = 4;
+constexpr int kFewThreads = 256;
+
+struct Few {
+  int n, C, d, bf16;
+  const uint16_t *X, *W;
+  long long ldx, sx, ldw, sw;
+  const int* y;
+  float2* part;             // [N][n][blocks]
+  float* zy;                // [N][n]
+  int* status;
+};
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)),
+        "l"(*reinterpret_cast<const uint64_t*>(&c)));
+  return *reinterpret_cast<const float2*>(&r);
+}
+
+template <int R>
+__global__ void __launch_bounds__(kFewThreads, 2) k_few_loss(const Few a) {
+  extern __shared__ __align__(16) unsigned char few_smem[];
+  __shared__ float2 s_part[kFewThreads / 32][R];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int worker = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int vecs = (a.d + 7) / 8;                               // of a row; the last one filled up with zeros
+  uint4* xs = reinterpret_cast<uint4*>(few_smem);               // [R][vecs]
+  const uint16_t* X = a.X + worker * a.sx;
+  const uint16_t* W = a.W + worker * a.sw;
+  auto vec_of = [&](const uint16_t* row, int v) {
+    if (8 * v + 8 <= a.d) return reinterpret_cast<const uint4*>(row)[v];
+    uint32_t u[4] = {0u, 0u, 0u, 0u};
+    for (int e = 0; 8 * v + e < a.d; ++e) u[e >> 1] |= static_cast<uint32_t>(row[8 * v + e]) << (16 * (e & 1));
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  };
+  for (int i = 0; i < R; ++i)
+    for (int v = tid; v < vecs; v += kFewThreads) xs[i * vecs + v] = vec_of(X + i * a.ldx, v);
+  if (blockIdx.x == 0 && worker == 0 && tid == 0) *a.status = 0;
+  __syncthreads();
+  float m[R], s[R];
+  int label[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    m[i] = -INFINITY;
+    s[i] = 0.f;
+    label[i] = a.y[static_cast<long long>(worker) * R + i];
+  }
+  const int warps = gridDim.x * (kFewThreads / 32);
+  for (long long c0 = static_cast<long long>(blockIdx.x * (kFewThreads / 32) + warp) * kFewCols; c0 < a.C;
+       c0 += static_cast<long long>(warps) * kFewCols) {
+    const uint16_t* row[kFewCols];                              // what lies beyond the last row is that row again
+#pragma unroll
+    for (int c = 0; c < kFewCols; ++c) row[c] = W + min(c0 + c, static_cast<long long>(a.C - 1)) * a.ldw;
+    float2 z[R][kFewCols];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) z[i][c] = make_float2(0.f, 0.f);
+    auto step = [&](const uint4 (&w)[kFewCols], int v) {
+      float2 wf[kFewCols][4];
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) {
+        wf[c][0] = unpack16(w[c].x, a.bf16), wf[c][1] = unpack16(w[c].y, a.bf16);
+        wf[c][2] = unpack16(w[c].z, a.bf16), wf[c][3] = unpack16(w[c].w, a.bf16);
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const uint4 x = xs[i * vecs + v];
+        const float2 xf[4] = {unpack16(x.x, a.bf16), unpack16(x.y, a.bf16), unpack16(x.z, a.bf16), unpack16(x.w, a.bf16)};
+#pragma unroll
+        for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[i][c] = fma2(xf[e], wf[c][e], z[i][c]);
+      }
+    };
+    int v = lane;
+    for (; v + 32 < a.d / 8; v += 64) {                         // two vectors of each row in flight
+      uint4 w0[kFewCols], w1[kFewCols];
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) {
+        w0[c] = __ldcs(reinterpret_cast<const uint4*>(row[c]) + v);
+        w1[c] = __ldcs(reinterpret_cast<const uint4*>(row[c]) + v + 32);
+      }
+      step(w0, v);
+      step(w1, v + 32);
+    }
+    for (; v < vecs; v += 32) {
+      uint4 w0[kFewCols];
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) w0[c] = vec_of(row[c], v);
+      step(w0, v);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) {
+        float t = z[i][c].x + z[i][c].y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (c0 + c < a.C) {
+          if (c0 + c == label[i] && lane == 0) a.zy[static_cast<long long>(worker) * R + i] = t;
+          const float top = fmaxf(m[i], t);
+          if (top > -INFINITY) s[i] = s[i] * ex2((m[i] - top) * kLog2e) + ex2((t - top) * kLog2e);
+          else s[i] += t != t ? t : 0.f;                        // -inf adds nothing, NaN goes on
+          m[i] = top;
+        }
+      }
+  }
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < R; ++i) s_part[warp][i] = make_float2(m[i], s[i]);
+  __syncthreads();
+  if (tid < R) {
+    float mm = -INFINITY, ss = 0.f;
+    for (int w = 0; w < kFewThreads / 32; ++w) join(mm, ss, s_part[w][tid].x, s_part[w][tid].y);
+    a.part[(static_cast<long long>(worker) * R + tid) * gridDim.x + blockIdx.x] = make_float2(mm, ss);
+  }
+}
+
 // ---- after ---------------------------------------------------------------------------
 constexpr int kLossWarps = 4;
 
 // A warp joins a row's parts.
 __global__ void __launch_bounds__(kLossWarps * 32)
-    k_finish_loss(const float2* part, int slots, const float* zy, const float* zy_sum, const int* perm, const int* nv, int n,
-                  float* loss, float* lse, const int* status) {
+    k_finish_loss(const float2* part, int slots, const float* zy, const float* zy_sum, const int* perm, const int* nv, const int* y,
+                  int n, int C, float* loss, float* lse, const int* status) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int worker = blockIdx.y, lane = threadIdx.x & 31, row = blockIdx.x * kLossWarps + (threadIdx.x >> 5);
   const long long wn = static_cast<long long>(worker) * n;
-  if (row >= nv[worker]) return;
+  if (row >= (nv ? nv[worker] : n)) return;
+  if (y) {                                                     // no rows were listed: each row's own label
+    const int label = y[wn + row];
+    if (!labelled(label, C)) {
+      if (lane == 0) {
+        loss[wn + row] = label < 0 ? 0.f : __int_as_float(0x7fc00000);
+        lse[wn + row] = 0.f;
+      }
+      return;
+    }
+  }
   part += (wn + row) * slots;
   float m = -INFINITY, s = 0.f;
 #pragma unroll 4
@@ -893,7 +1031,7 @@ __global__ void __launch_bounds__(kLossWarps * 32)
   const float z = zy[wn + row], off = z - zy_sum[wn + row];
   float l = dead ? __int_as_float(0x7fc00000) : m + logf(s);
   if (fabsf(off) < 1e-2f) l += ex2((z - l) * kLog2e) * off;      // no correction of what is not finite
-  const int at = perm[wn + row];
+  const int at = perm ? perm[wn + row] : row;
   lse[wn + at] = l;
   loss[wn + at] = l - z;
 }
@@ -1018,6 +1156,8 @@ constexpr long long kMaxRows = 1 << 24, kMaxVocab = 1 << 28, kMaxD = 1 << 20;
 constexpr int kMaxWorkers = 1024;
 
 // Where everything lies in the workspace, and how the vocabulary is cut.
+constexpr int kFewBlocks = 304;                // of all workers: two on each SM
+
 struct Plan {
   long long n_pad, ldc, ld_acc;
   int tiles_m, tiles_v, tiles_d, splits;
@@ -1064,7 +1204,7 @@ Plan plan_common(const Shape& s) {
 
 Plan plan_forward(const Shape& s) {
   Plan p = plan_common(s);
-  p.part = take(p.end, 8 * static_cast<size_t>(s.N) * p.tiles_v * s.n);
+  p.part = take(p.end, 8 * static_cast<size_t>(s.N) * std::max(p.tiles_v, kFewBlocks / s.N + 1) * s.n);
   p.zy = take(p.end, 8 * static_cast<size_t>(s.N) * s.n);
   return p;
 }
@@ -1186,6 +1326,30 @@ cudaError_t launch_prepare(Launch& l, Prep q) {
   return cudaLaunchKernelEx(l.at(dim3((q.n + q.per_block - 1) / q.per_block, q.N), kPrepThreads, 0, false), k_prepare, q);
 }
 
+// X's rows have to fit into shared memory twice over an SM.
+bool few(const Shape& s) { return s.n <= kFewRows && s.n * up(s.d, 8) * 2 <= 48 << 10; }
+
+int few_blocks(const Shape& s) {
+  const long long most = (s.C + kFewCols * (kFewThreads / 32) - 1) / (kFewCols * (kFewThreads / 32));
+  return static_cast<int>(std::max<long long>(1, std::min<long long>(most, kFewBlocks / s.N)));
+}
+
+cudaError_t forward_few(Launch& l, const Shape& s, bool bf16, const Matrix& X, const Matrix& W, const int32_t* y, float* loss,
+                        float* lse, float2* part, float* zy, int* status) {
+  Few a = {static_cast<int>(s.n), static_cast<int>(s.C), static_cast<int>(s.d), bf16, static_cast<const uint16_t*>(X.p),
+           static_cast<const uint16_t*>(W.p), X.ld, s.N == 1 ? 0 : X.stride, W.ld, s.N == 1 ? 0 : W.stride, y, part, zy, status};
+  const int blocks = few_blocks(s);
+  const size_t smem = static_cast<size_t>(s.n * up(s.d, 8) * 2);
+  cudaLaunchConfig_t* cfg = l.at(dim3(blocks, s.N), kFewThreads, smem, false);
+  cudaError_t e = s.n == 1 ? cudaLaunchKernelEx(cfg, k_few_loss<1>, a) : s.n == 2 ? cudaLaunchKernelEx(cfg, k_few_loss<2>, a)
+                : s.n == 3 ? cudaLaunchKernelEx(cfg, k_few_loss<3>, a) : cudaLaunchKernelEx(cfg, k_few_loss<4>, a);
+  if (e == cudaSuccess)
+    e = cudaLaunchKernelEx(l.at(dim3(1, s.N), kLossWarps * 32, 0, false), k_finish_loss, static_cast<const float2*>(part), blocks,
+                           static_cast<const float*>(zy), static_cast<const float*>(zy), static_cast<const int*>(nullptr),
+                           static_cast<const int*>(nullptr), y, a.n, a.C, loss, lse, static_cast<const int*>(status));
+  return e;
+}
+
 #define XENT_CHECK(f)                                                                                             \
   if (!sizes_ok(s))                                                                                               \
     return reject(ASAP_ERR_ARG, f ": need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256");       \
@@ -1211,6 +1375,13 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   if (st != ASAP_OK) return st;
   unsigned char* w = static_cast<unsigned char*>(ws);
   const bool bf16 = dtype == ASAP_BF16;
+  Launch l;
+  l.stream = stream;
+  if (few(s)) {
+    const cudaError_t e = forward_few(l, s, bf16, X, W, y, loss, lse, reinterpret_cast<float2*>(w + p.part),
+                                      reinterpret_cast<float*>(w + p.zy), static_cast<int*>(ws));
+    return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
+  }
   CUtensorMap tx, txc, tw;
   if (!encode(dev, &tx, bf16, X.p, s.d, s.n, s.N, X.ld, stride_of(X, s.n, s.N)) ||
       !encode(dev, &txc, bf16, w + p.xc, s.d, p.n_pad, s.N, p.ldc, p.n_pad * p.ldc) ||
@@ -1230,14 +1401,12 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   a.X = q.X, a.ldx = X.ld, a.sx = q.sx;
   a.W = static_cast<const uint16_t*>(W.p), a.ldw = W.ld, a.sw = s.N == 1 ? 0 : W.stride;
   a.part = reinterpret_cast<float2*>(w + p.part), a.zy = reinterpret_cast<float*>(w + p.zy), a.status = q.status;
-  Launch l;
-  l.stream = stream;
   cudaError_t e = launch_prepare(l, q);
   if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw, tw, tw);
   if (e == cudaSuccess)
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
                            static_cast<const float2*>(a.part), p.tiles_v, static_cast<const float*>(a.zy), static_cast<const float*>(a.zy + s.N * s.n), a.perm, a.nv,
-                           a.n, loss, lse, static_cast<const int*>(a.status));
+                           static_cast<const int*>(nullptr), a.n, a.C, loss, lse, static_cast<const int*>(a.status));
   return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
 }
 

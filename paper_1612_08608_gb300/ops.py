@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+from array import array
 from typing import Optional, Sequence
 
 import torch
@@ -15,6 +16,7 @@ from ._lib import load_library
 from .api import AsapError
 
 DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_FLOATS, _HALVES = set(DTYPE), {torch.bfloat16, torch.float16}
 
 
 def _call(status: int):
@@ -45,34 +47,43 @@ def _launch(device: torch.device, fn, *args):
             _call(fn(*args, stream))
 
 
-def _pointers(tensors):
-    return (C.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
+def _pointers(tensors) -> array:
+    return array("Q", [0 if t is None else t.data_ptr() for t in tensors])
 
 
-def _tensor_list(name: str, tensors, like: Sequence[torch.Tensor]):
+def _at(values: Optional[array]) -> Optional[int]:
+    """The address of an array's elements (the array has to outlive its use)."""
+    return None if values is None else values.buffer_info()[0]
+
+
+def _tensor_list(name: str, tensors, like: Sequence[torch.Tensor], dtypes):
+    """Checks a list that goes with the gradients: contiguous tensors (or None) of their sizes, of the given types."""
     if len(tensors) != len(like):
         raise ValueError("%s: %d tensors for %d gradients" % (name, len(tensors), len(like)))
-    if any(t is not None and (t.numel() != g.numel() or not t.is_contiguous()) for t, g in zip(tensors, like)):
+    held = [(t, g) for t, g in zip(tensors, like) if t is not None]
+    if [t.numel() for t, _ in held] != [g.numel() for _, g in held] or not all([t.is_contiguous() for t, _ in held]):
         raise ValueError("%s: need contiguous tensors of the gradients' sizes" % name)
+    if not {t.dtype for t, _ in held} <= dtypes:
+        raise ValueError("%s: need %s" % (name, " or ".join(sorted(map(str, dtypes)))))
 
 
 def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
     """What asap_clip_grads and asap_sgd_clipped share, as (device, arrays, groups, n_groups, norms, workspace)."""
     device = _one_device([*grads, *others])
-    dtypes = [DTYPE.get(g.dtype, -1) for g in grads]
-    if -1 in dtypes:
-        raise ValueError("gradients are float32, bfloat16 or float16")
+    try:
+        dtypes = array("i", [DTYPE[g.dtype] for g in grads])
+    except KeyError:
+        raise ValueError("gradients are float32, bfloat16 or float16") from None
     if not all([g.is_contiguous() for g in grads]):
         raise ValueError("need contiguous gradients")
-    T = len(grads)
     if groups is not None:
-        if len(groups) != T:
-            raise ValueError("%d groups for %d gradients" % (len(groups), T))
+        if len(groups) != len(grads):
+            raise ValueError("%d groups for %d gradients" % (len(groups), len(grads)))
         if n_groups is None:
             n_groups = max(groups) + 1
         if min(groups) < 0 or max(groups) >= n_groups:
             raise ValueError("groups: need numbers from 0 to %d" % (n_groups - 1))
-        groups = (C.c_int32 * T)(*groups)
+        groups = array("i", groups)
     elif n_groups is None:
         n_groups = 1
     if norms is None:
@@ -80,8 +91,7 @@ def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
     elif norms.dtype != torch.float32 or norms.shape != (n_groups,) or not norms.is_contiguous() or norms.device != device:
         raise ValueError("norms: need %d contiguous float32 on %s" % (n_groups, device))
     workspace = _workspace(workspace, 0 if workspace is not None else clip_workspace(n_groups), device)
-    arrays = (_pointers(grads), (C.c_int64 * T)(*[g.numel() for g in grads]), (C.c_int32 * T)(*dtypes))
-    return device, arrays, groups, n_groups, norms, workspace
+    return device, (_pointers(grads), array("q", [g.numel() for g in grads]), dtypes), groups, n_groups, norms, workspace
 
 
 def _workspace(workspace: Optional[torch.Tensor], size: int, device) -> torch.Tensor:
@@ -187,16 +197,15 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
     is not scaled."""
     if not grads:
         raise ValueError("no gradients")
-    only = out is None and max_norm == float("inf")
     if out is not None:
-        _tensor_list("out", out, grads)
-        if any(o.dtype != g.dtype for o, g in zip(out, grads)):
+        _tensor_list("out", out, grads, _FLOATS)
+        if None in [None if o is None else 0 for o in out] or [o.dtype for o in out] != [g.dtype for g in grads]:
             raise ValueError("out: need the gradients' types")
     device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
                                                                                        workspace, out or ())
-    dst = None if only else ptrs if out is None else _pointers(out)
-    _launch(device, load_library().asap_clip_grads, len(grads), ptrs, dst, numel, dtypes, groups, n_groups, max_norm,
-            norms.data_ptr(), workspace.data_ptr(), workspace.numel())
+    dst = _pointers(out) if out is not None else None if max_norm == float("inf") else ptrs
+    _launch(device, load_library().asap_clip_grads, len(grads), _at(ptrs), _at(dst), _at(numel), _at(dtypes), _at(groups),
+            n_groups, max_norm, norms.data_ptr(), workspace.data_ptr(), workspace.numel())
     return norms
 
 
@@ -209,21 +218,20 @@ def sgd_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: 
     whose norm is not finite takes no step.  Returns the norms."""
     if not grads:
         raise ValueError("no gradients")
-    _tensor_list("params", params, grads)
-    if any(p.dtype != torch.float32 for p in params):
-        raise ValueError("params: need float32")
+    _tensor_list("params", params, grads, {torch.float32})
+    if None in [None if p is None else 0 for p in params]:
+        raise ValueError("params: need a tensor for every gradient")
     held = []
     if copies is not None:
-        _tensor_list("copies", copies, grads)
+        _tensor_list("copies", copies, grads, _HALVES)
         held = [c for c in copies if c is not None]
-        if any(c.dtype not in (torch.bfloat16, torch.float16) for c in held):
-            raise ValueError("copies: need bfloat16 or float16")
     device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
                                                                                        workspace, [*params, *held])
-    cptr = ctype = None
+    w = _pointers(params)
+    c = ctypes = None
     if copies is not None:
-        cptr = _pointers(copies)
-        ctype = (C.c_int32 * len(copies))(*[0 if c is None else DTYPE[c.dtype] for c in copies])
-    _launch(device, load_library().asap_sgd_clipped, len(grads), _pointers(params), cptr, ctype, ptrs, numel, dtypes, groups,
-            n_groups, max_norm, lr, l2, norms.data_ptr(), workspace.data_ptr(), workspace.numel())
+        c = _pointers(copies)
+        ctypes = array("i", [0 if t is None else DTYPE[t.dtype] for t in copies])
+    _launch(device, load_library().asap_sgd_clipped, len(grads), _at(w), _at(c), _at(ctypes), _at(ptrs), _at(numel), _at(dtypes),
+            _at(groups), n_groups, max_norm, lr, l2, norms.data_ptr(), workspace.data_ptr(), workspace.numel())
     return norms

@@ -95,6 +95,46 @@ def test_odd_sizes_in_padded_rows(N, n, C, d, dtype):
     _check(X, W, y, g, *_run(X, W, y, g))
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("N,n,C,d,pad", [(1, 1, 50001, 256, 0), (1, 2, 3000, 1001, 2), (3, 3, 999, 8, 0), (2, 4, 4099, 777, 1),
+                                         (300, 1, 17, 40, 0), (1, 4, 40000, 2056, 0), (1, 5, 40000, 72, 0), (1, 1, 3, 24577, 0)])
+def test_few_rows(N, n, C, d, pad, dtype):
+    X, W, y, g = _inputs(N, n, C, d, dtype, seed=C, pad=pad)
+    y[0, n - 1] = C - 1
+    _check(X, W, y, g, *_run(X, W, y, g))
+    if n > 1:
+        y[0, 0], y[N - 1, 1] = -5, -1                           # and rows without a label among them
+        X[0, 0] = float("nan")
+        _check(X, W, y, g, *_run(X, W, y, g))
+
+
+def test_infinite_logits():
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    for n in (2, 40):
+        X, W, y, g = _inputs(1, n, 700, 64, "bfloat16", seed=2)
+        ref = ops.softmax_xent(X, W, y)[1]
+        y.fill_(300)
+        X[0, 0, 0] = 1.0
+        W[0, 5:9] = 0.0
+        W[0, 5:9, 0] = float("-inf")                            # a masked class: exp of it is 0, where x_0 > 0
+        X[0, 1:, 0] = X[0, 1:, 0].abs() + 0.5
+        loss, lse = ops.softmax_xent(X, W, y)
+        z = X[0].double() @ torch.where(torch.isinf(W[0]), 0.0, W[0].double()).T
+        z[:, 5:9] = float("-inf")
+        want = torch.logsumexp(z, 1)
+        assert bool(((lse[0] - want).abs() <= 1e-4).all())      # 64 products of a few units, 2^-23 each
+        W[0, 11, 0] = float("inf")                              # an infinite one leaves no finite loss
+        loss, lse = ops.softmax_xent(X, W, y)
+        assert not bool(torch.isfinite(loss).any())
+        W[0, 11, 0] = float("nan")
+        assert bool(torch.isnan(ops.softmax_xent(X, W, y)[1]).all())
+        W[:] = 0.0
+        W[0, :, 0] = float("-inf")                              # nothing is left of the vocabulary
+        assert not bool(torch.isfinite(ops.softmax_xent(X, W, y)[0]).any())
+
+
 @pytest.mark.parametrize("drop", [0.3, 0.97, 1.0])
 @pytest.mark.parametrize("N,n,C,d", [(1, 40, 100, 64), (3, 600, 900, 136), (2, 1111, 300, 77)])
 def test_rows_without_a_label(N, n, C, d, drop):
