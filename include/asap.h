@@ -512,12 +512,13 @@ asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int back
  * scale of a group whose norm is not finite is 1.  A group without elements has
  * the norm 0.  max_norm > 0, infinity included.
  * The arrays are host arrays, read during the call; grads, out, norms_out
- * (n_groups floats) and the workspace (asap_clip_workspace bytes, 8-byte
+ * (n_groups floats) and the workspace (asap_clip_workspace bytes, 16-byte
  * aligned, any contents) are device memory of the current device.  Tensors need
- * their type's alignment; those that lie alike within 16 bytes in grads and out
- * are moved fastest.  Calls that share a workspace must not overlap on the GPU.
- * The same inputs give the same bits.  Async on cuda_stream (NULL: legacy default
- * stream); it may be captured.  Allocates no device memory. */
+ * their type's alignment; those that lie alike within 128 bytes in grads and
+ * out are moved fastest.  Calls that share a workspace must not overlap on the GPU.
+ * The same tensors give the same bits; copies of them at addresses that lie otherwise
+ * within 128 bytes may be summed in another order.  Async on cuda_stream (NULL: legacy
+ * default stream); it may be captured.  Allocates no device memory. */
 asap_status asap_clip_grads(int count, const void* const* grads, void* const* out, const int64_t* numel,
                             const int32_t* dtypes, const int32_t* groups, int n_groups, float max_norm,
                             float* norms_out, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
@@ -536,7 +537,7 @@ asap_status asap_sgd_clipped(int count, float* const* params, void* const* copie
                              float* norms_out, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
 
 /* Bytes of workspace of the two calls above.  Host only. */
-asap_status asap_clip_workspace(int n_groups, uint64_t* bytes);
+asap_status asap_clip_workspace(int count, int n_groups, uint64_t* bytes);
 
 const char* asap_last_error(const asap_ctx* ctx);
 const char* asap_version(void);

@@ -63,7 +63,7 @@ SIGNATURES = {
     "asap_xent_backward": (C.c_int, [C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int64, _P,
                                      C.c_int64, C.c_int64, _P, _P, _P, _P, C.c_int64, C.c_int64, _P, C.c_int64,
                                      C.c_int64, _P, C.c_uint64, _P]),
-    "asap_clip_workspace": (C.c_int, [C.c_int, C.POINTER(C.c_uint64)]),
+    "asap_clip_workspace": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_uint64)]),
     "asap_clip_grads": (C.c_int, [C.c_int, _P, _P, _P, _P, _P, C.c_int, C.c_float, _P, _P, C.c_uint64, _P]),
     "asap_sgd_clipped": (C.c_int, [C.c_int, _P, _P, _P, _P, _P, _P, _P, C.c_int, C.c_float, C.c_float, C.c_float, _P, _P,
                                    C.c_uint64, _P]),

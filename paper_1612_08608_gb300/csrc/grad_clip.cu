@@ -7,18 +7,20 @@
 //   out     = scale_k g                                   (clip)
 //   w       = (1 - lr l2) w - lr scale_k g; copy = w      (step)
 //
-// Two launches: every gradient is read for the norms, then once more to be
-// scaled.  Tensors are cut into chunks of kChunk elements, sorted by group; block
-// b takes the chunks [b per, (b + 1) per), so that the partial sum of (block b,
-// group k) has the slot b + k: no two share one, a group's lie side by side, and
-// no ticket, atomic or clearing of the workspace is needed.  Each block of the
-// second launch adds up the slots of the groups that it meets, all in the same
-// order.  The second launch walks the chunks backwards: what the first one read
-// last is still in L2.
+// Every gradient is read for the norms, then once more to be scaled.  Tensors lie
+// sorted by group and are cut into chunks; a block sums one chunk into a slot of
+// its own (no ticket, no atomic, nothing to clear), and a second launch scales
+// smaller chunks, a block each, from the last to the first: what the first launch
+// read last is still in L2.  A block for each chunk, not a resident grid that walks
+// them: copying 2 GB goes at 7.1 TB/s so, at 6.3 to 6.7 the other way.  The slots of a
+// group are added up by every block that scales a part of it, or, where there are more
+// than a block's threads (kFewSlots), by a launch between the two: 32 groups of 62 slots 66
+// us without it, 67 with it; one of 16384, 4580 and 914.
 //
-// Squares are added in fp32 per thread and chunk, the chunks' sums as
-// float-float pairs, and the threads' sums in fp64.  Where fp32 squares overflow
-// or vanish, the thread adds its elements of the chunk again in fp64.
+// Squares are added in fp32, at most 16 in a row, and those sums as float-float pairs.
+// Where fp32 squares overflow or vanish, the thread adds its elements of the chunk
+// again in fp64.  (This GPU's fp64 pipe is narrow: with fp64 from the threads' sums on, the
+// sums of a block's 256 threads and a square root in each took 2.5 us.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -40,10 +42,13 @@ namespace {
 using namespace asap;
 
 constexpr int kThreads = 256;
-constexpr int kBlocksPerSm = 6;
-constexpr int kChunk = 16384;                // elements
-constexpr int kStepUnroll = 2;             // groups of eight elements of the step in flight, a thread
-constexpr int kMaxBlocks = 1024;             // slots for partial sums: this and one for each group
+constexpr int kNormThreads = 1024;
+constexpr int kChunk = 8192;                  // elements that a block scales, and at least those whose squares it sums
+constexpr int kLongChunk = 32768;             // ... where there are kLongChunks of them or more
+constexpr int kLongChunks = 2432;
+constexpr int kMostChunks = 16384;            // chunks of squares, besides one for each tensor
+constexpr int kFewSlots = 256;                // a group's slots that every scaling block adds up itself
+constexpr int kStepUnroll = 2;                // groups of eight elements of the step in flight, a thread
 constexpr int kMaxGroups = 65536;
 
 struct Tensor {
@@ -51,13 +56,23 @@ struct Tensor {
   void* a;               // clip: the scaled gradient; step: the fp32 parameters
   void* c;               // step: their 16-bit copy (may be NULL)
   long long n;
-  int chunk0;            // number of the first chunk
+  int sum0, scale0;      // numbers of its first chunks
   int group;
-  int gchunk0, gchunk1;  // chunks of the whole group
+  int gsum0, gsum1;      // chunks of squares of the whole group
   unsigned char type;    // of g (and of a, for a clip)
-  unsigned char ctype;   // of c
-  unsigned char head;    // elements before the first chunk's vectors
-  unsigned char vec;     // a and c are aligned there too
+  unsigned char ctype;   // of c; kLoose: a and c are not aligned where g is
+  unsigned char sum_head, scale_head;   // elements before the first chunk's vectors
+};
+constexpr int kLoose = 128;
+
+struct Pair {
+  float hi, lo;
+};
+
+// A sum of squares: what fp32 held of it, and what it did not.
+struct __align__(16) Sum {
+  Pair p;
+  double wide;
 };
 
 // The tables travel as kernel arguments: nothing is copied, and a captured
@@ -66,29 +81,47 @@ template <int T>
 struct Args {
   Tensor t[T];
   int count;
-  int chunk_begin, chunk_end;   // of this launch
-  int per;                      // chunks per block
-  int first_block;
+  int first;                    // this launch's first chunk
+  int sum_size;                 // elements of a chunk of squares
   float max_norm;
   float decay, lr;              // step
-  double* partial;
+  Sum* partial;                 // a slot for each chunk of squares
+  float* scales;                // [groups], or NULL: add up the slots
   float* norms;
 };
 
 constexpr int kSmallTable = 32, kLargeTable = 576;
 static_assert(sizeof(Args<kLargeTable>) <= 32764, "kernel arguments");
 
-struct Pair {
-  float hi, lo;
-};
-
 // Knuth's two-sum: the rounding error of the high parts' sum is kept in lo.
-__device__ __forceinline__ Pair pair_add(Pair a, float b) {
-  const float s = a.hi + b;
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b) {
+  const float s = a.hi + b.hi;
   const float bv = s - a.hi;
-  const float e = ((a.hi - (s - bv)) + (b - bv)) + a.lo;
+  const float e = ((a.hi - (s - bv)) + (b.hi - bv)) + (a.lo + b.lo);
   const float hi = s + e;
   return Pair{hi, e - (hi - s)};
+}
+
+__device__ __forceinline__ bool any_wide(const Sum& v) { return __any_sync(0xffffffffu, __double_as_longlong(v.wide) != 0); }
+
+__device__ __forceinline__ Sum warp_sum(Sum v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    v.p = pair_add(v.p, Pair{__shfl_xor_sync(0xffffffffu, v.p.hi, o), __shfl_xor_sync(0xffffffffu, v.p.lo, o)});
+  if (any_wide(v))
+    for (int o = 16; o > 0; o >>= 1) v.wide += __shfl_xor_sync(0xffffffffu, v.wide, o);
+  return v;
+}
+
+// Over a block of K threads in a fixed order; valid in thread 0.
+template <int K>
+__device__ __forceinline__ Sum block_sum(Sum v, Sum* red) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  v = warp_sum(v);
+  if (lane == 0) red[warp] = v;
+  __syncthreads();
+  if (warp == 0) v = warp_sum(lane < K / 32 ? red[lane] : Sum{{0.f, 0.f}, 0.0});
+  return v;
 }
 
 __device__ __forceinline__ float as_float(float v) { return v; }
@@ -123,89 +156,79 @@ __device__ __forceinline__ void store_vec(E* p, const Vec<E>& v) {
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&v);
 }
 
-// Elements [begin, end) of chunk j of a tensor; the part from `body` on starts
-// at a 16-byte boundary of g.
+// Elements [begin, end) of a tensor's chunk j of `size`; the part from `body` on starts
+// at the boundary that its head leads to.
 struct Range {
   long long begin, body, end;
 };
 
-__device__ __forceinline__ Range chunk_range(const Tensor& t, int j) {
+__device__ __forceinline__ Range chunk_range(const Tensor& t, int j, int size, int head) {
   Range r;
-  const long long aligned = t.head + static_cast<long long>(j) * kChunk;
+  const long long aligned = head + static_cast<long long>(j) * size;
   r.begin = j ? aligned : 0;
   r.body = aligned < t.n ? aligned : t.n;
-  r.end = aligned + kChunk < t.n ? aligned + kChunk : t.n;
+  r.end = aligned + size < t.n ? aligned + size : t.n;
   return r;
 }
 
+// The tensor of a chunk, by its number among those of squares or of scaling.
 template <int T>
-__device__ __forceinline__ int tensor_of(const Args<T>& a, int chunk) {
+__device__ __forceinline__ int tensor_of(const Args<T>& a, int chunk, int Tensor::*first) {
   int lo = 0, hi = a.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (a.t[mid].chunk0 <= chunk) lo = mid; else hi = mid - 1;
+    if (a.t[mid].*first <= chunk) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
 
-// Sum over the block in a fixed order, in every thread.
-__device__ __forceinline__ double block_sum(double v, double* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double t = 0.0;
-  for (int w = 0; w < kThreads / 32; ++w) t += red[w];
-  return t;
-}
-
 // This thread's sum of squares of a chunk.
 template <typename E>
-__device__ __forceinline__ double chunk_squares(const E* g, const Range& r, Pair& total) {
-  constexpr int kN = Vec<E>::kN;
+__device__ __forceinline__ Sum chunk_squares(const E* g, const Range& r) {
+  constexpr int kN = Vec<E>::kN, kU = 8;
   const long long nv = (r.end - r.body) / kN;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  bool seen = false;     // an element that is not zero
+  bool seen = false, narrow = true;      // an element that is not zero; fp32 holds the squares
+  Pair total{0.f, 0.f};
   const E* body = g + r.body;
   long long v = threadIdx.x;
-  for (; v + 3 * kThreads < nv; v += 4 * kThreads) {
-    Vec<E> x[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = load_vec(body + (v + u * kThreads) * kN);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        const float f = as_float(x[u].e[e]);
-        s[u] = fmaf(f, f, s[u]);
-        seen |= f != 0.f;
-      }
-  }
-  for (; v < nv; v += kThreads) {
-    const Vec<E> x = load_vec(body + v * kN);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const Vec<E>& x, int u) {
 #pragma unroll
     for (int e = 0; e < kN; ++e) {
       const float f = as_float(x.e[e]);
-      s[e & 3] = fmaf(f, f, s[e & 3]);
+      s[(u + e) & 3] = fmaf(f, f, s[(u + e) & 3]);
       seen |= f != 0.f;
     }
+  };
+  auto take = [&] {                      // a short sum into the long one
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    // What squares below 2^-126 lose is nothing beside a sum above 2^-100; as many
+    // sums below 2^80 as there can be do not overflow.
+    narrow = narrow && (!seen || (sum >= 0x1p-100f && sum < 0x1p+80f));
+    total = pair_add(total, Pair{sum, 0.f});
+    s[0] = s[1] = s[2] = s[3] = 0.f;
+    seen = false;
+  };
+  for (; v + (kU - 1) * kThreads < nv; v += kU * kThreads) {
+    Vec<E> x[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) x[u] = load_vec(body + (v + u * kThreads) * kN);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) add(x[u], u);
+    take();
   }
+#pragma unroll 4
+  for (; v < nv; v += kThreads) add(load_vec(body + v * kN), 0);
   const long long tail = r.body + nv * kN;
-  const long long loose = (r.body - r.begin) + (r.end - tail);     // fewer than 2 kN
+  const long long loose = (r.body - r.begin) + (r.end - tail);     // fewer than 64 + kN
   const long long at = threadIdx.x < r.body - r.begin ? r.begin + threadIdx.x : tail + (threadIdx.x - (r.body - r.begin));
   if (threadIdx.x < loose) {
     const float f = as_float(g[at]);
     s[0] = fmaf(f, f, s[0]);
     seen |= f != 0.f;
   }
-  const float sum = (s[0] + s[1]) + (s[2] + s[3]);
-  // What squares below 2^-126 lose is nothing beside a sum above 2^-100, and the
-  // sums of 2^27 chunks below 2^100 do not overflow.
-  if (!seen || (sum >= 0x1p-100f && sum < 0x1p+100f)) {
-    total = pair_add(total, sum);
-    return 0.0;
-  }
+  take();
+  if (narrow) return Sum{total, 0.0};
   double w = 0.0;
   for (v = threadIdx.x; v < nv; v += kThreads)
     for (int e = 0; e < kN; ++e) {
@@ -216,56 +239,59 @@ __device__ __forceinline__ double chunk_squares(const E* g, const Range& r, Pair
     const double f = as_float(g[at]);
     w += f * f;
   }
-  return w;
+  return Sum{{0.f, 0.f}, w};
 }
 
 template <int T>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_grad_squares(const __grid_constant__ Args<T> a) {
-  __shared__ double red[kThreads / 32];
+__global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant__ Args<T> a) {
+  __shared__ Sum red[kThreads / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int b = a.first_block + blockIdx.x;
-  const int begin = max(a.chunk_begin, b * a.per);
-  const int end = static_cast<int>(min(static_cast<long long>(a.chunk_end), (b + 1LL) * a.per));
-  if (begin >= end) return;
-  int ti = tensor_of(a, begin);
-  Pair total{0.f, 0.f};
-  double wide = 0.0;
-  auto flush = [&](int i) {
-    const Tensor& t = a.t[i];
-    const double sum = block_sum(static_cast<double>(total.hi) + static_cast<double>(total.lo) + wide, red);
-    // the part of this (block, group) that an earlier launch summed
-    const bool more = max(b * a.per, t.gchunk0) < a.chunk_begin;
-    if (threadIdx.x == 0) a.partial[b + t.group] = more ? a.partial[b + t.group] + sum : sum;
-    total = Pair{0.f, 0.f};
-    wide = 0.0;
-  };
-  for (int c = begin; c < end; ++c) {
-    while (ti + 1 < a.count && a.t[ti + 1].chunk0 <= c) {
-      if (a.t[ti + 1].group != a.t[ti].group) flush(ti);
-      ++ti;
-    }
-    const Tensor& t = a.t[ti];
-    const Range r = chunk_range(t, c - t.chunk0);
-    switch (t.type) {
-      case ASAP_F32: wide += chunk_squares(static_cast<const float*>(t.g), r, total); break;
-      case ASAP_BF16: wide += chunk_squares(static_cast<const __nv_bfloat16*>(t.g), r, total); break;
-      default: wide += chunk_squares(static_cast<const __half*>(t.g), r, total); break;
-    }
+  const int c = a.first + blockIdx.x;
+  const Tensor& t = a.t[tensor_of(a, c, &Tensor::sum0)];
+  const Range r = chunk_range(t, c - t.sum0, a.sum_size, t.sum_head);
+  Sum w;
+  switch (t.type) {
+    case ASAP_F32: w = chunk_squares(static_cast<const float*>(t.g), r); break;
+    case ASAP_BF16: w = chunk_squares(static_cast<const __nv_bfloat16*>(t.g), r); break;
+    default: w = chunk_squares(static_cast<const __half*>(t.g), r); break;
   }
-  flush(ti);
+  w = block_sum<kThreads>(w, red);
+  if (threadIdx.x == 0) a.partial[c] = w;
 }
 
-// The norm of a group, the same in every thread and block.
-template <int T>
-__device__ __forceinline__ float group_norm(const Args<T>& a, const Tensor& t, double* red) {
-  double v = 0.0;
-  const int b1 = (t.gchunk1 - 1) / a.per;
-  for (int b = t.gchunk0 / a.per + threadIdx.x; b <= b1; b += kThreads) v += __ldcg(a.partial + b + t.group);
-  return static_cast<float>(sqrt(block_sum(v, red)));
+// The norm of the group with slots [from, to), the same in every block and launch; valid in thread 0.
+template <int K>
+__device__ __forceinline__ float group_norm(const Sum* partial, int from, int to, Sum* red) {
+  Sum v = {{0.f, 0.f}, 0.0};
+#pragma unroll 4
+  for (int c = from + threadIdx.x; c < to; c += K) {
+    const uint4 u = __ldcg(reinterpret_cast<const uint4*>(partial + c));
+    v.p = pair_add(v.p, Pair{__uint_as_float(u.x), __uint_as_float(u.y)});
+    if (u.z | u.w) v.wide += __hiloint2double(static_cast<int>(u.w), static_cast<int>(u.z));
+  }
+  v = block_sum<K>(v, red);
+  if (threadIdx.x != 0) return 0.f;
+  return static_cast<float>(sqrt(static_cast<double>(v.p.hi) + static_cast<double>(v.p.lo) + v.wide));
 }
 
 __device__ __forceinline__ float group_scale(float norm, float max_norm) {
   return norm > max_norm && norm < INFINITY ? max_norm / norm : 1.f;
+}
+
+// A block for each tensor that begins a group: the group's norm, and its scale
+// (0: the norm is not finite, nothing is to be done with it).
+template <int T>
+__global__ void __launch_bounds__(kNormThreads) k_grad_norms(const __grid_constant__ Args<T> a) {
+  __shared__ Sum red[kNormThreads / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Tensor& t = a.t[blockIdx.x];
+  if (t.sum0 != t.gsum0) return;
+  const float norm = group_norm<kNormThreads>(a.partial, t.gsum0, t.gsum1, red);
+  if (threadIdx.x == 0) {
+    a.norms[t.group] = norm;
+    if (a.scales) a.scales[t.group] = norm < INFINITY ? group_scale(norm, a.max_norm) : 0.f;
+  }
 }
 
 template <typename E>
@@ -273,7 +299,7 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, const Range& r, flo
   constexpr int kN = Vec<E>::kN;
   const E* g = static_cast<const E*>(t.g);
   E* o = static_cast<E*>(t.a);
-  if (!t.vec) {
+  if (t.ctype & kLoose) {
     for (long long i = r.begin + threadIdx.x; i < r.end; i += kThreads) o[i] = from_float<E>(as_float(g[i]) * scale);
     return;
   }
@@ -339,7 +365,7 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Range& r, floa
     w[i] = x;
     if (kCopy) c[i] = from_float<H>(x);
   };
-  if (!t.vec) {
+  if (t.ctype & kLoose) {
     for (long long i = r.begin + threadIdx.x; i < r.end; i += kThreads) one(i);
     return;
   }
@@ -379,49 +405,47 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Range& r, floa
 template <typename E>
 __device__ __forceinline__ void step_any(const Tensor& t, const Range& r, float decay, float rate) {
   if (!t.c) step_chunk<E, __nv_bfloat16, false>(t, r, decay, rate);
-  else if (t.ctype == ASAP_BF16) step_chunk<E, __nv_bfloat16, true>(t, r, decay, rate);
+  else if ((t.ctype & ~kLoose) == ASAP_BF16) step_chunk<E, __nv_bfloat16, true>(t, r, decay, rate);
   else step_chunk<E, __half, true>(t, r, decay, rate);
 }
 
 enum Mode { kNormOnly, kClip, kStep };
 
 template <int T, int M>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_grad_apply(const __grid_constant__ Args<T> a) {
-  __shared__ double red[kThreads / 32];
-  const int b = a.first_block + blockIdx.x;
-  const int begin = max(a.chunk_begin, b * a.per);
-  const int end = static_cast<int>(min(static_cast<long long>(a.chunk_end), (b + 1LL) * a.per));
-  if (begin >= end) return;
-  int ti = tensor_of(a, end - 1);
+__global__ void __launch_bounds__(kThreads) k_grad_apply(const __grid_constant__ Args<T> a) {
+  __shared__ Sum red[kThreads / 32];
+  __shared__ float s_scale;
+  const int c = a.first + static_cast<int>(gridDim.x - 1 - blockIdx.x);
+  const Tensor& t = a.t[tensor_of(a, c, &Tensor::scale0)];
+  const Range r = chunk_range(t, c - t.scale0, kChunk, t.scale_head);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  int group = -1;
-  float scale = 1.f;
-  bool skip = false;
-  for (int c = end - 1; c >= begin; --c) {
-    while (a.t[ti].chunk0 > c) --ti;
-    const Tensor& t = a.t[ti];
-    if (t.group != group) {
-      group = t.group;
-      const float norm = group_norm(a, t, red);
-      scale = group_scale(norm, a.max_norm);
-      skip = M == kNormOnly || (M == kStep && !(norm < INFINITY));   // a gradient that is not finite takes no step
+  float scale;
+  if (a.scales) {
+    scale = __ldcg(a.scales + t.group);
+  } else {
+    const float norm = group_norm<kThreads>(a.partial, t.gsum0, t.gsum1, red);
+    if (threadIdx.x == 0) {
+      s_scale = norm < INFINITY ? group_scale(norm, a.max_norm) : 0.f;
       // the block with the group's first chunk reports its norm
-      if (t.gchunk0 >= b * a.per && threadIdx.x == 0) a.norms[group] = norm;
+      if (t.sum0 == t.gsum0 && c == t.scale0) a.norms[t.group] = norm;
     }
-    if (skip || (M == kClip && scale == 1.f && t.a == t.g)) continue;
-    const Range r = chunk_range(t, c - t.chunk0);
-    if (M == kClip) {
-      switch (t.type) {
-        case ASAP_F32: scale_chunk<float>(t, r, scale); break;
-        case ASAP_BF16: scale_chunk<__nv_bfloat16>(t, r, scale); break;
-        default: scale_chunk<__half>(t, r, scale); break;
-      }
-    } else if (M == kStep) {
-      switch (t.type) {
-        case ASAP_F32: step_any<float>(t, r, a.decay, a.lr * scale); break;
-        case ASAP_BF16: step_any<__nv_bfloat16>(t, r, a.decay, a.lr * scale); break;
-        default: step_any<__half>(t, r, a.decay, a.lr * scale); break;
-      }
+    __syncthreads();
+    scale = s_scale;
+  }
+  if (M == kClip) {
+    if (scale == 0.f) scale = 1.f;                      // not finite: as it is
+    if (scale == 1.f && t.a == t.g) return;
+    switch (t.type) {
+      case ASAP_F32: scale_chunk<float>(t, r, scale); break;
+      case ASAP_BF16: scale_chunk<__nv_bfloat16>(t, r, scale); break;
+      default: scale_chunk<__half>(t, r, scale); break;
+    }
+  } else {
+    if (scale == 0.f) return;                           // not finite: no step
+    switch (t.type) {
+      case ASAP_F32: step_any<float>(t, r, a.decay, a.lr * scale); break;
+      case ASAP_BF16: step_any<__nv_bfloat16>(t, r, a.decay, a.lr * scale); break;
+      default: step_any<__half>(t, r, a.decay, a.lr * scale); break;
     }
   }
 }
@@ -451,7 +475,10 @@ struct Call {
   int mode;
 };
 
-size_t workspace_of(int n_groups) { return 8 * (static_cast<size_t>(kMaxBlocks) + static_cast<size_t>(n_groups)); }
+// A slot for each chunk of squares, a scale for each group.
+size_t workspace_of(int count, int n_groups) {
+  return sizeof(Sum) * (static_cast<size_t>(kMostChunks) + static_cast<size_t>(count)) + 4 * static_cast<size_t>(n_groups);
+}
 
 // Written ranges must not meet each other, nor a gradient other than the one
 // that the same tensor is scaled in place from.
@@ -490,50 +517,61 @@ bool ranges_meet(const Call& k) {
 }
 
 template <int T>
-cudaError_t launch(const Call& k, const std::vector<Tensor>& tensors, int chunks, int per) {
+cudaError_t launch(const Call& k, const std::vector<Tensor>& tensors, int sums, int sum_size, int blocks, int slots) {
   Args<T> a;
-  a.per = per;
+  a.sum_size = sum_size;
   a.max_norm = k.max_norm;
   a.decay = k.decay;
   a.lr = k.lr;
-  a.partial = static_cast<double*>(k.workspace);
+  a.partial = static_cast<Sum*>(k.workspace);
   a.norms = k.norms;
+  a.scales = nullptr;
+  const bool between = k.mode == kNormOnly || slots > kFewSlots;
+  if (between && k.mode != kNormOnly)
+    a.scales = reinterpret_cast<float*>(a.partial + kMostChunks + static_cast<size_t>(k.count));
   const int total = static_cast<int>(tensors.size());
   const int parts = (total + T - 1) / T;
-  for (int pass = 0; pass < 2; ++pass)
-    for (int q = 0; q < parts; ++q) {
-      const int part = pass ? parts - 1 - q : q;     // the second pass goes backwards
-      const int t0 = part * T;
+  bool chained = false;                              // the launch before it is all that this one waits for
+  auto go = [&](auto kernel, int threads, int part, int grid, int first) {
+    const int t0 = part * T;
+    if (parts > 1 || !chained) {
       a.count = std::min(T, total - t0);
       std::copy(tensors.begin() + t0, tensors.begin() + t0 + a.count, a.t);
-      a.chunk_begin = a.t[0].chunk0;
-      a.chunk_end = t0 + a.count < total ? tensors[t0 + a.count].chunk0 : chunks;
-      a.first_block = a.chunk_begin / per;
-      const int blocks = (a.chunk_end - 1) / per - a.first_block + 1;
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(blocks);
-      cfg.blockDim = dim3(kThreads);
-      cfg.stream = k.stream;
-      cudaLaunchAttribute attr[1];
-      attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      attr[0].val.programmaticStreamSerializationAllowed = 1;
-      cfg.attrs = attr;
-      cfg.numAttrs = pass && q == 0 ? 1 : 0;         // the first launch after the squares' last
-      cudaError_t e;
-      if (pass == 0) e = cudaLaunchKernelEx(&cfg, k_grad_squares<T>, a);
-      else if (k.mode == kNormOnly) e = cudaLaunchKernelEx(&cfg, k_grad_apply<T, kNormOnly>, a);
-      else if (k.mode == kClip) e = cudaLaunchKernelEx(&cfg, k_grad_apply<T, kClip>, a);
-      else e = cudaLaunchKernelEx(&cfg, k_grad_apply<T, kStep>, a);
-      if (e != cudaSuccess) return e;
     }
-  return cudaSuccess;
+    a.first = first;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = k.stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = chained ? 1 : 0;
+    chained = parts == 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+  };
+  auto end_of = [&](int part, int Tensor::*first, int all) {
+    return (part + 1) * T < total ? tensors[(part + 1) * T].*first : all;
+  };
+  cudaError_t e = cudaSuccess;
+  for (int q = 0; q < parts && e == cudaSuccess; ++q) {
+    const int first = tensors[q * T].sum0;
+    e = go(k_grad_squares<T>, kThreads, q, end_of(q, &Tensor::sum0, sums) - first, first);
+  }
+  for (int q = 0; between && q < parts && e == cudaSuccess; ++q) e = go(k_grad_norms<T>, kNormThreads, q, std::min(T, total - q * T), 0);
+  for (int q = parts - 1; k.mode != kNormOnly && q >= 0 && e == cudaSuccess; --q) {
+    const int first = tensors[q * T].scale0, grid = end_of(q, &Tensor::scale0, blocks) - first;
+    e = k.mode == kClip ? go(k_grad_apply<T, kClip>, kThreads, q, grid, first) : go(k_grad_apply<T, kStep>, kThreads, q, grid, first);
+  }
+  return e;
 }
 
 asap_status run(const Call& k, const char* const* why) {
   if (k.count < 0 || k.n_groups < 1 || k.n_groups > kMaxGroups) return reject(why[0]);
   if (!k.norms || !k.workspace || (k.count > 0 && (!k.grads || !k.numel || !k.dtypes || (k.mode != kNormOnly && !k.a))))
     return reject(why[1]);
-  if (k.workspace_bytes < workspace_of(k.n_groups) || (reinterpret_cast<uintptr_t>(k.workspace) & 7u) ||
+  if (k.workspace_bytes < workspace_of(k.count, k.n_groups) || (reinterpret_cast<uintptr_t>(k.workspace) & 15u) ||
       (reinterpret_cast<uintptr_t>(k.norms) & 3u))
     return reject(why[2]);
   if (!(k.max_norm > 0.f)) return reject(why[3]);
@@ -541,7 +579,7 @@ asap_status run(const Call& k, const char* const* why) {
   order.reserve(k.count);
   std::vector<char> has(k.n_groups, 0);
   bool sorted = true;
-  long long chunks = 0;
+  double elements = 0;
   for (int i = 0; i < k.count; ++i) {
     const int type = k.dtypes[i], group = k.groups ? k.groups[i] : 0;
     if (type != ASAP_F32 && type != ASAP_BF16 && type != ASAP_F16) return reject(why[4]);
@@ -560,12 +598,17 @@ asap_status run(const Call& k, const char* const* why) {
     }
     if (low) return reject(why[7]);
     if (!order.empty() && k.groups && k.groups[order.back()] > group) sorted = false;
+    elements += static_cast<double>(k.numel[i]);
     has[group] = 1;
     order.push_back(i);
   }
   if (k.mode != kNormOnly && ranges_meet(k)) return reject(why[8]);
   if (!sorted)
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return k.groups[x] < k.groups[y]; });
+  long long sum_size = kChunk;
+  while (elements / static_cast<double>(sum_size) > (sum_size < kLongChunk ? kLongChunks : kMostChunks)) sum_size *= 2;
+  if (sum_size > (1 << 30)) return reject(why[6]);
+  long long sums = 0, blocks = 0;
   std::vector<Tensor> tensors(order.size());
   for (size_t j = 0; j < order.size(); ++j) {
     const int i = order[j];
@@ -578,31 +621,43 @@ asap_status run(const Call& k, const char* const* why) {
     t.type = static_cast<unsigned char>(k.dtypes[i]);
     t.ctype = static_cast<unsigned char>(t.c ? k.cdtypes[i] : 0);
     const int es = bytes_of(t.type);
-    // The first element from which g and whatever the second pass moves beside it
-    // are aligned (the step takes eight elements at a time); none: g's own boundary.
+    // The first element at a whole line of g; and that from which g and whatever the second
+    // launch moves beside it lie at whole lines, or are aligned to what a thread moves (the step takes eight
+    // elements at a time); none: g's own boundary, and the second launch goes one by one.
     const uintptr_t g = reinterpret_cast<uintptr_t>(t.g), w = reinterpret_cast<uintptr_t>(t.a),
                     c = reinterpret_cast<uintptr_t>(t.c);
-    auto aligned = [&](uintptr_t h) {
-      if (k.mode != kStep) return ((g + h * es) & 15u) == 0 && (k.mode == kNormOnly || ((w + h * es) & 15u) == 0);
-      return ((g + h * es) & (8 * es - 1)) == 0 && ((w + h * 4) & 31u) == 0 && (!t.c || ((c + h * 2) & 15u) == 0);
+    auto aligned = [&](uintptr_t h, bool lines) {
+      const uintptr_t line = 127, g_at = lines ? line : (k.mode == kStep ? 8 * es - 1 : 15);
+      if ((g + h * es) & g_at) return false;
+      if (k.mode == kNormOnly) return true;
+      if (k.mode == kClip) return ((w + h * es) & (lines ? line : 15)) == 0;
+      return ((w + h * 4) & (lines ? line : 31)) == 0 && (!t.c || ((c + h * 2) & (lines ? line : 15)) == 0);
     };
-    uintptr_t head = 0;
-    while (head < 16 && !aligned(head)) ++head;
-    t.vec = head < 16;
-    if (!t.vec) head = ((16 - (g & 15u)) & 15u) / es;
-    t.head = static_cast<unsigned char>(std::min<long long>(static_cast<long long>(head), t.n));
-    t.chunk0 = static_cast<int>(chunks);
-    chunks += std::max<long long>(1, (t.n - t.head + kChunk - 1) / kChunk);
-    if (chunks > INT32_MAX / 2) return reject(why[6]);
+    uintptr_t head = 64;
+    for (int lines = 1; lines >= 0 && head == 64; --lines)
+      for (head = 0; head < 64 && !aligned(head, lines != 0);) ++head;
+    if (head == 64) {
+      t.ctype |= kLoose;
+      head = 0;
+    }
+    t.sum_head = static_cast<unsigned char>(std::min<long long>(static_cast<long long>(((128 - (g & 127u)) & 127u) / es), t.n));
+    t.scale_head = static_cast<unsigned char>(std::min<long long>(static_cast<long long>(head), t.n));
+    t.sum0 = static_cast<int>(sums);
+    t.scale0 = static_cast<int>(blocks);
+    sums += std::max<long long>(1, (t.n - t.sum_head + sum_size - 1) / sum_size);
+    blocks += std::max<long long>(1, (t.n - t.scale_head + kChunk - 1) / kChunk);
+    if (blocks > INT32_MAX) return reject(why[6]);
   }
+  int slots = 0;                                     // of the largest group
   for (size_t j = 0; j < tensors.size();) {
     size_t e = j;
     while (e < tensors.size() && tensors[e].group == tensors[j].group) ++e;
-    const int c1 = e < tensors.size() ? tensors[e].chunk0 : static_cast<int>(chunks);
-    const int c0 = tensors[j].chunk0;
+    const int c1 = e < tensors.size() ? tensors[e].sum0 : static_cast<int>(sums);
+    const int c0 = tensors[j].sum0;
+    slots = std::max(slots, c1 - c0);
     for (; j < e; ++j) {
-      tensors[j].gchunk0 = c0;
-      tensors[j].gchunk1 = c1;
+      tensors[j].gsum0 = c0;
+      tensors[j].gsum1 = c1;
     }
   }
   // groups without an element have the norm 0
@@ -615,16 +670,9 @@ asap_status run(const Call& k, const char* const* why) {
       break;
     }
   if (tensors.empty()) return ASAP_OK;
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
-    set_thread_error("no usable current device");
-    return ASAP_ERR_CUDA;
-  }
-  const int blocks = std::min(kMaxBlocks, kBlocksPerSm * sms);
-  const int per = static_cast<int>((chunks + blocks - 1) / blocks);
-  const cudaError_t e = tensors.size() <= kSmallTable ? launch<kSmallTable>(k, tensors, static_cast<int>(chunks), per)
-                                                      : launch<kLargeTable>(k, tensors, static_cast<int>(chunks), per);
+  const int s = static_cast<int>(sums), size = static_cast<int>(sum_size), b = static_cast<int>(blocks);
+  const cudaError_t e = tensors.size() <= kSmallTable ? launch<kSmallTable>(k, tensors, s, size, b, slots)
+                                                      : launch<kLargeTable>(k, tensors, s, size, b, slots);
   if (e != cudaSuccess) {
     cudaGetLastError();
     set_thread_error(cudaGetErrorString(e));
@@ -653,10 +701,10 @@ asap_status guarded(const Call& k, const char* const* why) {
 
 }  // namespace
 
-extern "C" asap_status asap_clip_workspace(int n_groups, uint64_t* bytes) {
-  if (!bytes || n_groups < 1 || n_groups > kMaxGroups)
-    return reject("asap_clip_workspace: need bytes and 1 <= n_groups <= 65536");
-  *bytes = workspace_of(n_groups);
+extern "C" asap_status asap_clip_workspace(int count, int n_groups, uint64_t* bytes) {
+  if (!bytes || count < 0 || n_groups < 1 || n_groups > kMaxGroups)
+    return reject("asap_clip_workspace: need bytes, count >= 0 and 1 <= n_groups <= 65536");
+  *bytes = workspace_of(count, n_groups);
   return ASAP_OK;
 }
 

@@ -359,7 +359,8 @@ struct Walk {
         }
         continue;
       }
-      int t = at;
+      // The residual goes backwards: what the logits (or a piece before) read last is still in L2.
+      int t = M == kResidual ? end - 1 - at : at;
       at += step;
       const int tiles_n = M == kGrads ? a.tiles_d : a.tiles_v;
       const int tiles_m = dw ? a.tiles_v : row_tiles;
@@ -1466,13 +1467,14 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
   Launch l;
   l.stream = stream;
   cudaError_t e = launch_prepare(l, q);
-  for (long long v0 = 0; v0 < s.C && e == cudaSuccess; v0 += p.piece) {
+  const long long last = (s.C - 1) / p.piece * p.piece, r_rows = up(s.n, kTileK);
+  for (long long v0 = last; v0 >= 0 && e == cudaSuccess; v0 -= p.piece) {      // from the last: see Walk
     a.v0 = static_cast<int>(v0);
     a.width = static_cast<int>(std::min<long long>(p.piece, s.C - v0));
-    a.first = v0 == 0;
+    a.first = v0 == last;
     CUtensorMap tr, tro;
-    if (!encode(dev, &tr, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece) ||
-        !encode(dev, &tro, bf16, w + p.R, a.width, p.n_pad, s.N, p.piece, p.n_pad * p.piece, true))
+    if (!encode(dev, &tr, bf16, w + p.R, a.width, r_rows, s.N, p.piece, p.n_pad * p.piece) ||
+        !encode(dev, &tro, bf16, w + p.R, a.width, r_rows, s.N, p.piece, p.n_pad * p.piece, true))
       return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
     a.tiles_v = (a.width + kTile - 1) / kTile;
     e = launch_gemm<kResidual>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * a.tiles_v, tx, txc, tw, tr, tro, tro);

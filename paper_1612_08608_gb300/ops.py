@@ -26,13 +26,10 @@ def _call(status: int):
 
 
 def _one_device(tensors) -> torch.device:
-    devices = {t.device for t in tensors}
-    if len(devices) != 1:
-        raise ValueError("tensors on more than one device: %s" % sorted(map(str, devices)))
-    device = devices.pop()
-    if device.type != "cuda":
-        raise ValueError("need CUDA tensors, got %s" % device)
-    return device
+    index = tensors[0].get_device()              # -1: not on a GPU
+    if index < 0 or [t.get_device() for t in tensors] != [index] * len(tensors):
+        raise ValueError("need CUDA tensors on one device, got %s" % sorted({str(t.device) for t in tensors}))
+    return tensors[0].device
 
 
 def _launch(device: torch.device, fn, *args):
@@ -56,18 +53,15 @@ def _at(values: Optional[array]) -> Optional[int]:
     return None if values is None else values.buffer_info()[0]
 
 
-def _tensor_list(name: str, tensors, like: Sequence[torch.Tensor], dtypes):
-    """Checks a list that goes with the gradients: contiguous tensors (or None) of their sizes, of the given types."""
-    if len(tensors) != len(like):
-        raise ValueError("%s: %d tensors for %d gradients" % (name, len(tensors), len(like)))
-    held = [(t, g) for t, g in zip(tensors, like) if t is not None]
-    if [t.numel() for t, _ in held] != [g.numel() for _, g in held] or not all([t.is_contiguous() for t, _ in held]):
-        raise ValueError("%s: need contiguous tensors of the gradients' sizes" % name)
-    if not {t.dtype for t, _ in held} <= dtypes:
+def _tensor_list(name: str, tensors, sizes, dtypes):
+    """Checks a list that goes with the gradients: contiguous tensors of their sizes, of the given types."""
+    if [t.numel() for t in tensors] != sizes or not all([t.is_contiguous() for t in tensors]):
+        raise ValueError("%s: need a contiguous tensor of each gradient's size" % name)
+    if not {t.dtype for t in tensors} <= dtypes:
         raise ValueError("%s: need %s" % (name, " or ".join(sorted(map(str, dtypes)))))
 
 
-def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
+def _clip_arguments(grads, sizes, groups, n_groups, norms, workspace, others=()):
     """What asap_clip_grads and asap_sgd_clipped share, as (device, arrays, groups, n_groups, norms, workspace)."""
     device = _one_device([*grads, *others])
     try:
@@ -90,8 +84,8 @@ def _clip_arguments(grads, groups, n_groups, norms, workspace, others=()):
         norms = torch.empty(n_groups, dtype=torch.float32, device=device)
     elif norms.dtype != torch.float32 or norms.shape != (n_groups,) or not norms.is_contiguous() or norms.device != device:
         raise ValueError("norms: need %d contiguous float32 on %s" % (n_groups, device))
-    workspace = _workspace(workspace, 0 if workspace is not None else clip_workspace(n_groups), device)
-    return device, (_pointers(grads), array("q", [g.numel() for g in grads]), dtypes), groups, n_groups, norms, workspace
+    workspace = _workspace(workspace, 0 if workspace is not None else clip_workspace(len(grads), n_groups), device)
+    return device, (_pointers(grads), array("q", sizes), dtypes), groups, n_groups, norms, workspace
 
 
 def _workspace(workspace: Optional[torch.Tensor], size: int, device) -> torch.Tensor:
@@ -122,6 +116,8 @@ def _matrix(name: str, t: torch.Tensor):
 def _like(t: torch.Tensor) -> torch.Tensor:
     """An empty tensor of t's shape in rows of a multiple of 16 bytes."""
     d = t.shape[-1]
+    if d % 8 == 0:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
     return torch.empty((*t.shape[:-1], (d + 7) // 8 * 8), dtype=t.dtype, device=t.device)[..., :d]
 
 
@@ -180,10 +176,10 @@ def softmax_xent_grad(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor, lse: to
 
 
 @functools.lru_cache(maxsize=64)
-def clip_workspace(n_groups: int = 1) -> int:
-    """Bytes of workspace of clip_grads and sgd_step."""
+def clip_workspace(count: int, n_groups: int = 1) -> int:
+    """Bytes of workspace of clip_grads and sgd_step for `count` tensors in `n_groups` groups."""
     size = C.c_uint64()
-    _call(load_library().asap_clip_workspace(n_groups, C.byref(size)))
+    _call(load_library().asap_clip_workspace(count, n_groups, C.byref(size)))
     return size.value
 
 
@@ -197,11 +193,12 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
     is not scaled."""
     if not grads:
         raise ValueError("no gradients")
+    sizes = [g.numel() for g in grads]
     if out is not None:
-        _tensor_list("out", out, grads, _FLOATS)
-        if None in [None if o is None else 0 for o in out] or [o.dtype for o in out] != [g.dtype for g in grads]:
+        _tensor_list("out", out, sizes, _FLOATS)
+        if [o.dtype for o in out] != [g.dtype for g in grads]:
             raise ValueError("out: need the gradients' types")
-    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
+    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, sizes, groups, n_groups, norms,
                                                                                        workspace, out or ())
     dst = _pointers(out) if out is not None else None if max_norm == float("inf") else ptrs
     _launch(device, load_library().asap_clip_grads, len(grads), _at(ptrs), _at(dst), _at(numel), _at(dtypes), _at(groups),
@@ -218,14 +215,16 @@ def sgd_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: 
     whose norm is not finite takes no step.  Returns the norms."""
     if not grads:
         raise ValueError("no gradients")
-    _tensor_list("params", params, grads, {torch.float32})
-    if None in [None if p is None else 0 for p in params]:
-        raise ValueError("params: need a tensor for every gradient")
+    sizes = [g.numel() for g in grads]
+    _tensor_list("params", params, sizes, {torch.float32})
     held = []
     if copies is not None:
-        _tensor_list("copies", copies, grads, _HALVES)
         held = [c for c in copies if c is not None]
-    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, groups, n_groups, norms,
+        of = sizes if len(held) == len(sizes) else [n for n, c in zip(sizes, copies) if c is not None]
+        if len(copies) != len(sizes):
+            raise ValueError("copies: %d for %d gradients" % (len(copies), len(sizes)))
+        _tensor_list("copies", held, of, _HALVES)
+    device, (ptrs, numel, dtypes), groups, n_groups, norms, workspace = _clip_arguments(grads, sizes, groups, n_groups, norms,
                                                                                        workspace, [*params, *held])
     w = _pointers(params)
     c = ctypes = None

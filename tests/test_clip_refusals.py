@@ -34,7 +34,7 @@ def _clip(lib, grads=(0x10000,), out=(0x20000,), numel=(8,), dtypes=(0,), groups
 @pytest.mark.parametrize("change,word", [
     (dict(count=-1), b"count"), (dict(n_groups=0), b"n_groups"), (dict(n_groups=65537), b"n_groups"),
     (dict(norms=None), b"NULL"), (dict(ws=None), b"NULL"), (dict(grads=(None,)), b"NULL"), (dict(out=(None,)), b"NULL"),
-    (dict(size=8), b"workspace"), (dict(ws=0x40004), b"workspace"), (dict(norms=0x30002), b"norms"),
+    (dict(size=8), b"workspace"), (dict(ws=0x40008), b"workspace"), (dict(norms=0x30002), b"norms"),
     (dict(max_norm=0.0), b"max_norm"), (dict(max_norm=-1.0), b"max_norm"), (dict(max_norm=float("nan")), b"max_norm"),
     (dict(dtypes=(3,)), b"type"), (dict(dtypes=(-1,)), b"type"), (dict(groups=(1,)), b"group"), (dict(groups=(-1,)), b"group"),
     (dict(numel=(-1,)), b"count"), (dict(numel=((1 << 40) + 1,)), b"count"),
@@ -71,12 +71,13 @@ def test_sgd_refuses(lib, change, word):
 
 def test_workspace_sizes(lib):
     v = C.c_uint64()
-    assert lib.asap_clip_workspace(1, C.byref(v)) == 0 and v.value > 0
+    assert lib.asap_clip_workspace(1, 1, C.byref(v)) == 0 and v.value > 0
     one = v.value
-    assert lib.asap_clip_workspace(65536, C.byref(v)) == 0 and v.value > one
+    assert lib.asap_clip_workspace(1, 65536, C.byref(v)) == 0 and v.value > one
     for k in (0, -1, 65537):
-        assert lib.asap_clip_workspace(k, C.byref(v)) == 1
-    assert lib.asap_clip_workspace(1, None) == 1
+        assert lib.asap_clip_workspace(1, k, C.byref(v)) == 1
+    assert lib.asap_clip_workspace(1, 1, None) == 1
+    assert lib.asap_clip_workspace(-1, 1, C.byref(v)) == 1
 
 
 def test_python_forms_refuse_what_they_cannot_pass_on(lib):

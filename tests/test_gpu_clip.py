@@ -73,9 +73,13 @@ def test_clip_against_the_definition(name, dtypes):
             assert all(abs(a - b) <= 12 * U * b for a, b in zip(got, norms_w)), (got, norms_w)
             for o, g, k in zip(out, grads, groups):
                 _close(o, g.double() * scale[k], g.dtype)
-            again = [g.clone() for g in grads]                            # in place, the same bits
-            assert torch.equal(ops.clip_grads(again, max_norm, groups=groups, n_groups=G), norms)
-            assert all(torch.equal(a, o) for a, o in zip(again, out))
+            # In place, on copies.  They lie at other addresses, by which elements are summed together: both norms
+            # are within 12 u of the definition's, and may differ in their last bit.
+            again = [g.clone() for g in grads]
+            got = ops.clip_grads(again, max_norm, groups=groups, n_groups=G).tolist()
+            assert all(abs(a - b) <= 12 * U * b for a, b in zip(got, norms_w)), (got, norms_w)
+            for a, g, k in zip(again, grads, groups):
+                _close(a, g.double() * scale[k], g.dtype)
             assert torch.equal(ops.clip_grads(grads, groups=groups, n_groups=G), norms)    # norms alone
 
 
@@ -163,7 +167,7 @@ def test_many_groups_and_the_same_bits_twice():
     groups = [(i * 31) % 999 for i in range(2000)]
     norms_w, scale = _want(grads, groups, 1000, 20.0)
     out = [torch.empty_like(g) for g in grads]
-    ws = torch.full((ops.clip_workspace(1000),), 255, dtype=torch.uint8, device="cuda")        # any contents
+    ws = torch.full((ops.clip_workspace(2000, 1000),), 255, dtype=torch.uint8, device="cuda")        # any contents
     norms = ops.clip_grads(grads, 20.0, out=out, groups=groups, n_groups=1000, workspace=ws)
     assert all(abs(a - b) <= 12 * U * b for a, b in zip(norms.tolist(), norms_w))
     for o, g, k in zip(out, grads, groups):
@@ -189,7 +193,7 @@ def test_streams_and_graphs():
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(out, want_out))
     # two graphs on one workspace, replayed in turn; inputs change between replays
-    ws = torch.empty(ops.clip_workspace(), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(ops.clip_workspace(3), dtype=torch.uint8, device="cuda")
     graphs, results = [], []
     for max_norm in (5.0, 50.0):
         o = [torch.empty_like(g) for g in grads]
