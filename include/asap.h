@@ -464,8 +464,8 @@ typedef enum {
  * Limits: 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer
  * than 10^9 tiles of 256 x 256 in N n x C, N n x d and N C x d.
  * workspace: at least asap_xent_workspace's `least` bytes, at a multiple of 256
- * bytes, any contents; outputs and workspace may not overlap each other or an
- * input.  All are device memory of the current device.  Calls that share a
+ * bytes, any contents; outputs and workspace, from their first to their last
+ * element, may not overlap each other or an input.  All are device memory of the current device.  Calls that share a
  * workspace must not overlap on the GPU.  The same call gives the same bits.
  * Async on cuda_stream (NULL: legacy default stream); it may be captured after a
  * first call on the device.  Allocates no device memory.  The kernel's waits are
@@ -483,7 +483,8 @@ asap_status asap_xent_forward(int N, int64_t n, int64_t C, int64_t d, int32_t dt
  * vocabulary at a time: R of one piece is held in the workspace, scaled so
  * that the largest |g| of a worker lies at 2^14, and rounded to `dtype`; so an
  * element of dX or dW is off by about one rounding of R's elements and one of its
- * own.  dX rows of rows left out are 0.  A workspace of `least` bytes takes pieces
+ * own.  dX rows of rows left out, and of those with
+ * y >= C, are 0.  A workspace of `least` bytes takes pieces
  * of 256 columns; more makes them wider, and fewer (asap_xent_workspace's `bytes`
  * is a good size; the width changes the order of dX's sums).  If a wait runs out,
  * dX and dW hold a NaN and the workspace's first int32 is ASAP_ERR_TIMEOUT.  The rest
@@ -509,7 +510,7 @@ asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int back
  * out NULL: only the norms.  out[i] == grads[i]: in place; written tensors may
  * not overlap each other or another gradient.  Sums are carried so that neither
  * their squares' overflow nor their underflow shows; out is rounded once.  The
- * scale of a group whose norm is not finite is 1.  A group without elements has
+ * scale of a group whose norm is not finite (in fp32) is 1.  A group without elements has
  * the norm 0.  max_norm > 0, infinity included.
  * The arrays are host arrays, read during the call; grads, out, norms_out
  * (n_groups floats) and the workspace (asap_clip_workspace bytes, 16-byte

@@ -274,12 +274,12 @@ __device__ __forceinline__ float group_norm(const Sum* partial, int from, int to
   return static_cast<float>(sqrt(static_cast<double>(v.p.hi) + static_cast<double>(v.p.lo) + v.wide));
 }
 
-__device__ __forceinline__ float group_scale(float norm, float max_norm) {
-  return norm > max_norm && norm < INFINITY ? max_norm / norm : 1.f;
-}
+__device__ __forceinline__ float group_scale(float norm, float max_norm) { return norm > max_norm ? max_norm / norm : 1.f; }
 
-// A block for each tensor that begins a group: the group's norm, and its scale
-// (0: the norm is not finite, nothing is to be done with it).
+// Nothing is scaled, no step taken, with a norm that is not finite.
+constexpr float kNotFinite = -1.f;
+
+// A block for each tensor that begins a group: the group's norm, and its scale.
 template <int T>
 __global__ void __launch_bounds__(kNormThreads) k_grad_norms(const __grid_constant__ Args<T> a) {
   __shared__ Sum red[kNormThreads / 32];
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kNormThreads) k_grad_norms(const __grid_consta
   const float norm = group_norm<kNormThreads>(a.partial, t.gsum0, t.gsum1, red);
   if (threadIdx.x == 0) {
     a.norms[t.group] = norm;
-    if (a.scales) a.scales[t.group] = norm < INFINITY ? group_scale(norm, a.max_norm) : 0.f;
+    if (a.scales) a.scales[t.group] = norm < INFINITY ? group_scale(norm, a.max_norm) : kNotFinite;
   }
 }
 
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_apply(const __grid_constant__
   } else {
     const float norm = group_norm<kThreads>(a.partial, t.gsum0, t.gsum1, red);
     if (threadIdx.x == 0) {
-      s_scale = norm < INFINITY ? group_scale(norm, a.max_norm) : 0.f;
+      s_scale = norm < INFINITY ? group_scale(norm, a.max_norm) : kNotFinite;
       // the block with the group's first chunk reports its norm
       if (t.sum0 == t.gsum0 && c == t.scale0) a.norms[t.group] = norm;
     }
@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_apply(const __grid_constant__
     scale = s_scale;
   }
   if (M == kClip) {
-    if (scale == 0.f) scale = 1.f;                      // not finite: as it is
+    if (scale == kNotFinite) scale = 1.f;
     if (scale == 1.f && t.a == t.g) return;
     switch (t.type) {
       case ASAP_F32: scale_chunk<float>(t, r, scale); break;
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_apply(const __grid_constant__
       default: scale_chunk<__half>(t, r, scale); break;
     }
   } else {
-    if (scale == 0.f) return;                           // not finite: no step
+    if (scale == kNotFinite) return;
     switch (t.type) {
       case ASAP_F32: step_any<float>(t, r, a.decay, a.lr * scale); break;
       case ASAP_BF16: step_any<__nv_bfloat16>(t, r, a.decay, a.lr * scale); break;

@@ -26,8 +26,9 @@
 // rows together if any is left out (so that what stands in the others, NaN even,
 // meets no product).  The logits of the labels are taken again, in fp32 arithmetic: the
 // tensor cores' sums are cut off after each step, which shows in the loss (d = 4096,
-// logits of 12: 3e-6 of it); k_finish_loss puts the label's term in lse right by it.  R is fp16 for fp16 operands (an MMA's have one type): it is
-// scaled by a power of two that brings the largest |g| near the top of the range.
+// logits of 12: 3e-6 of it); k_finish_loss puts the label's term in lse right by it.
+// R is of the operands' type (an MMA's have one): it is scaled so that the largest |g|
+// comes to lie near the top of fp16's range, on a value that rounding leaves alone.
 //
 // Every wait is time-limited.  One that runs out sets the workspace's status word; the
 // kernels after it do nothing but turn their outputs' first element into NaN.
@@ -1040,11 +1041,10 @@ __global__ void __launch_bounds__(kLossWarps * 32)
   }
   if (lane != 0) return;
   const bool dead = *static_cast<const volatile int*>(status) != 0;
-  // The label's own term, the largest of a confident row, is taken with its exact logit:
-  // d lse / d z_y = p_y.
-  const float z = zy[wn + row], off = z - zy_sum[wn + row];
+  // The label's own term, the largest of a confident row, is taken with its exact logit.
+  const float z = zy[wn + row], z_sum = zy_sum[wn + row], off = z - z_sum;
   float l = dead ? __int_as_float(0x7fc00000) : m + logf(s);
-  if (fabsf(off) < 1e-2f) l += ex2((z - l) * kLog2e) * off;      // no correction of what is not finite
+  if (off != 0.f && fabsf(off) < 64.f) l += log1pf(fminf(ex2((z_sum - l) * kLog2e), 1.f) * expm1f(off));
   const int at = perm ? perm[wn + row] : row;
   lse[wn + at] = l;
   loss[wn + at] = l - z;
@@ -1148,6 +1148,16 @@ asap_status device(Device* out) {
   }
   *out = d;
   return ASAP_OK;
+}
+
+// A launch that failed: after a reset of the device its kernels' settings are gone, and the next call makes them again.
+asap_status launch_error(const char* what, cudaError_t e) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    g_devices[dev].ready = false;
+  }
+  return cuda_error(what, e);
 }
 
 // [N][rows][inner] of 16-bit elements; boxes of 64 x 64 in 128-byte swizzle to load, of 32 x
@@ -1341,8 +1351,8 @@ cudaError_t launch_prepare(Launch& l, Prep q) {
   return cudaLaunchKernelEx(l.at(dim3((q.n + q.per_block - 1) / q.per_block, q.N), kPrepThreads, 0, false), k_prepare, q);
 }
 
-// X's rows have to fit into shared memory twice over an SM.
-bool few(const Shape& s) { return s.n <= kFewRows && s.n * up(s.d, 8) * 2 <= 48 << 10; }
+// X's rows have to fit, with the block's sums, into the 48 KB of shared memory that a launch has without asking.
+bool few(const Shape& s) { return s.n <= kFewRows && s.n * up(s.d, 8) * 2 <= 40 << 10; }
 
 int few_blocks(const Shape& s) {
   const long long most = (s.C + kFewCols * (kFewThreads / 32) - 1) / (kFewCols * (kFewThreads / 32));
@@ -1378,6 +1388,8 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   if (!matrix_ok(X, s.n, s.d, s.N) || !matrix_ok(W, s.C, s.d, s.N))
     return reject(ASAP_ERR_ARG, "asap_xent_forward: need X and W at multiples of 16 bytes, in rows of ld >= d elements "
                                 "and strides that are multiples of 8 elements");
+  if ((reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(loss) | reinterpret_cast<uintptr_t>(lse)) & 3u)
+    return reject(ASAP_ERR_ARG, "asap_xent_forward: need y, loss and lse at multiples of 4 bytes");
   const unsigned long long rows4 = 4ull * s.N * s.n;
   const Extent used[] = {extent(loss, rows4), extent(lse, rows4), extent(ws, ws_bytes), extent(X, s.n, s.d, s.N),
                          extent(W, s.C, s.d, s.N), extent(y, rows4)};
@@ -1395,7 +1407,7 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   if (few(s)) {
     const cudaError_t e = forward_few(l, s, bf16, X, W, y, loss, lse, reinterpret_cast<float2*>(w + p.part),
                                       reinterpret_cast<float*>(w + p.zy), static_cast<int*>(ws));
-    return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
+    return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_forward: launch failed", e);
   }
   CUtensorMap tx, txc, tw;
   if (!encode(dev, &tx, bf16, X.p, s.d, s.n, s.N, X.ld, stride_of(X, s.n, s.N)) ||
@@ -1422,7 +1434,7 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
                            static_cast<const float2*>(a.part), p.tiles_v, static_cast<const float*>(a.zy), static_cast<const float*>(a.zy + s.N * s.n), a.perm, a.nv,
                            static_cast<const int*>(nullptr), a.n, a.C, loss, lse, static_cast<const int*>(a.status));
-  return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_forward: launch failed", e);
+  return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_forward: launch failed", e);
 }
 
 asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W, const int32_t* y, const float* lse,
@@ -1435,6 +1447,8 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
       (dW.p && !matrix_ok(dW, s.C, s.d, s.N)))
     return reject(ASAP_ERR_ARG, "asap_xent_backward: need X, W, dX and dW at multiples of 16 bytes, in rows of ld >= d "
                                 "elements and strides that are multiples of 8 elements");
+  if ((reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(g)) & 3u)
+    return reject(ASAP_ERR_ARG, "asap_xent_backward: need y, lse and g at multiples of 4 bytes");
   const unsigned long long rows4 = 4ull * s.N * s.n;
   const Extent used[] = {extent(dX, s.n, s.d, s.N), extent(dW, s.C, s.d, s.N), extent(ws, ws_bytes), extent(X, s.n, s.d, s.N),
                          extent(W, s.C, s.d, s.N), extent(y, rows4), extent(lse, rows4), extent(g, rows4)};
@@ -1500,7 +1514,7 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
     e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N), 256, 0, false),
                            k_finish_dx, static_cast<const float*>(a.acc), p.splits, a.N, a.acc_rows, a.ld_acc, a.perm, a.nv,
                            a.scale, a.n, a.d, a.bf16, q.dX, q.lddx, q.sdx, static_cast<const int*>(a.status));
-  return e == cudaSuccess ? ASAP_OK : cuda_error("asap_xent_backward: launch failed", e);
+  return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_backward: launch failed", e);
 }
 
 }  // namespace

@@ -158,6 +158,38 @@ def test_gradients_that_are_not_finite(bad):
     assert bool((w[0] < 1).all()) and bool((w[1] == 1).all()) and bool((c[1] == 0).all())       # no step for group 1
 
 
+def test_a_scale_that_vanishes_is_still_a_scale():
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    g, w = [torch.full((3000,), 1e12, device="cuda")], [torch.ones(3000, device="cuda")]
+    out = [torch.full_like(g[0], float("nan"))]
+    ops.clip_grads(g, 1e-38, out=out)                            # 1e-38 / 5e13 is 0 in fp32
+    assert bool((out[0] == 0).all())
+    ops.sgd_step(w, g, 0.5, 1e-38, l2=0.5)
+    assert bool((w[0] == 0.75).all())                            # the shrink alone
+
+
+def test_tensors_beyond_32_bit_offsets():
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    n = 2 ** 31 + 70001
+    flat = torch.empty(n + 3, dtype=torch.float16, device="cuda")
+    for part in flat.split(2 ** 28):
+        part.fill_(0.25)
+    g = flat[3:]
+    g[-1], g[2 ** 31], g[2 ** 31 - 1] = 100.0, 7.0, 5.0
+    want = math.sqrt((n - 3) * 0.0625 + 1e4 + 49.0 + 25.0)
+    norms = ops.clip_grads([g, torch.ones(5, device="cuda")], want / 4, groups=[0, 1])
+    assert abs(norms[0].item() - want) <= 12 * U * want
+    head = float(torch.tensor(0.0625, dtype=torch.float16))      # 0.25 / 4 to within a rounding
+    for part in g.split(2 ** 28):
+        assert float(part.min()) >= head * (1 - 2.0 ** -10) and int((part > head * (1 + 2.0 ** -10)).sum()) <= 3
+    assert [float(g[i]) for i in (-1, 2 ** 31, 2 ** 31 - 1)] == [25.0, 1.75, 1.25]
+    assert float(flat[2]) == 0.25                                # what lies before it
+
+
 def test_many_groups_and_the_same_bits_twice():
     import torch
 
@@ -176,11 +208,12 @@ def test_many_groups_and_the_same_bits_twice():
         assert torch.equal(ops.clip_grads(grads, 20.0, out=out, groups=groups, n_groups=1000), norms)
 
 
-def test_streams_and_graphs():
+@pytest.mark.parametrize("tensors", [3, 50, 700])                 # a small table, a large one, two
+def test_streams_and_graphs(tensors):
     import torch
 
     from paper_1612_08608_gb300 import ops
-    grads = _grads([70000, 3, 16385], ["bfloat16", "float32"], 11)
+    grads = _grads([70000, 3, 16385] + [1 + (i * 53) % 900 for i in range(tensors - 3)], ["bfloat16", "float32"], 11)
     out = [torch.empty_like(g) for g in grads]
     want = ops.clip_grads(grads, 5.0, out=out).clone()
     want_out = [o.clone() for o in out]
@@ -193,7 +226,7 @@ def test_streams_and_graphs():
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(out, want_out))
     # two graphs on one workspace, replayed in turn; inputs change between replays
-    ws = torch.empty(ops.clip_workspace(3), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(ops.clip_workspace(tensors), dtype=torch.uint8, device="cuda")
     graphs, results = [], []
     for max_norm in (5.0, 50.0):
         o = [torch.empty_like(g) for g in grads]

@@ -97,7 +97,8 @@ def test_odd_sizes_in_padded_rows(N, n, C, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("N,n,C,d,pad", [(1, 1, 50001, 256, 0), (1, 2, 3000, 1001, 2), (3, 3, 999, 8, 0), (2, 4, 4099, 777, 1),
-                                         (300, 1, 17, 40, 0), (1, 4, 40000, 2056, 0), (1, 5, 40000, 72, 0), (1, 1, 3, 24577, 0)])
+                                         (300, 1, 17, 40, 0), (1, 4, 40000, 2056, 0), (1, 5, 40000, 72, 0), (1, 1, 3, 24577, 0),
+                                         (1, 1, 50, 20480, 0), (1, 4, 50, 5120, 0), (1, 1, 50, 24576, 0), (1, 2, 50, 12288, 0)])
 def test_few_rows(N, n, C, d, pad, dtype):
     X, W, y, g = _inputs(N, n, C, d, dtype, seed=C, pad=pad)
     y[0, n - 1] = C - 1
@@ -253,6 +254,59 @@ def test_what_lies_around_the_outputs_is_left_alone():
     assert torch.equal(dX, ref[0]) and torch.equal(dW, ref[1])
     assert bool((bx[:, 70:] == 7).all()) and bool((bx[:, :, 100:] == 7).all())
     assert bool((bw[:, 300:] == 7).all()) and bool((bw[:, :, 100:] == 7).all())
+
+
+def test_a_confident_row_with_huge_logits_has_no_loss():
+    # logits of some 1e5: the tensor cores' sums are off by tenths, the label's exact logit is not
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    for n in (1, 30):
+        X, W, y, g = _inputs(1, n, 400, 512, "bfloat16", seed=n)
+        y[0] = torch.arange(n, device="cuda").to(torch.int32)
+        X[0] = W[0, :n] * 512
+        W[0] *= 512
+        loss, lse = ops.softmax_xent(X, W, y)
+        z = X[0].double() @ W[0].double().T
+        own = z[torch.arange(n), y[0].long()]
+        other = z.scatter(1, y[0].long()[:, None], float("-inf")).max()
+        assert bool((own > 1e5).all()) and float(other) < float(own.min()) - 1e4
+        assert bool(((lse[0] - own).abs() <= 2.0 ** -22 * own).all())
+        assert bool((loss[0].abs() <= 2.0 ** -21 * own).all())
+
+
+def test_heads_beyond_32_bit_offsets():
+    # 600,000 classes of 4096: 2.46e9 elements, 4.9 GB each of W and dW
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    C, d = 600000, 4096
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    W = torch.empty((1, C, d), dtype=torch.bfloat16, device="cuda")
+    for part in W[0].split(50000):
+        part.copy_(torch.randn(part.shape, generator=gen, device="cuda") / 64)
+    edge = 2 ** 31 // d
+    for n in (3, 40):
+        X = torch.randn((1, n, d), generator=gen, device="cuda").bfloat16()
+        y = torch.randint(0, C, (1, n), generator=gen, device="cuda").to(torch.int32)
+        y[0, 0], y[0, 1], y[0, 2] = C - 1, edge, edge - 1
+        g = torch.full((1, n), 1.0 / n, device="cuda")
+        loss, lse, dX, dW = _run(X, W, y, g)
+        z = torch.cat([X[0].double() @ part.double().T for part in W[0].split(50000)], dim=1)
+        want = torch.logsumexp(z, 1)
+        tol = (d / 16 + 8) * 2.0 ** -23 * 60 + 2.0 ** -18        # magnitudes of a logit's products: 4096 / 64 x 0.64
+        assert bool(((lse[0] - want).abs() <= tol).all())
+        assert bool(((loss[0] - (want - z[torch.arange(n), y[0].long()])).abs() <= 2 * tol).all())
+        r = torch.exp(z - want[:, None])
+        r[torch.arange(n), y[0].long()] -= 1.0
+        r /= n
+        rows = torch.cat([torch.arange(300), torch.arange(edge - 200, edge + 200), torch.arange(C - 300, C)]).cuda()
+        dw, mag = r[:, rows].T @ X[0].double(), r[:, rows].abs().T @ X[0].double().abs()
+        assert bool(((dW[0, rows] - dw).abs() <= (2.0 ** -8 + 4 * tol) * mag + 2.0 ** -8 * dw.abs()).all())
+        dx = sum(r[:, i:i + 50000] @ W[0, i:i + 50000].double() for i in range(0, C, 50000))
+        mag = sum(r[:, i:i + 50000].abs() @ W[0, i:i + 50000].double().abs() for i in range(0, C, 50000))
+        assert bool(((dX[0] - dx).abs() <= (2.0 ** -8 + 4 * tol + C / 16 * 2.0 ** -23) * mag + 2.0 ** -8 * dx.abs()).all())
+        del z, r, dX, dW
 
 
 def test_streams_and_graphs():

@@ -42,7 +42,7 @@ BOTH = [(dict(N=0), b"N"), (dict(N=1025), b"N"), (dict(n=-1), b"n"), (dict(n=(1 
         (dict(ws=(1 << 32) + 256), b"overlap")]
 
 
-@pytest.mark.parametrize("change,word", BOTH + [(dict(loss=None), b"NULL"), (dict(loss=(5 << 32) + 4), b"overlap"),
+@pytest.mark.parametrize("change,word", BOTH + [(dict(loss=None), b"NULL"), (dict(y=(3 << 32) + 2), b"4 bytes"), (dict(lse=(5 << 32) + 1), b"4 bytes"), (dict(loss=(5 << 32) + 4), b"overlap"),
                                                 (dict(lse=3 << 32), b"overlap")])
 def test_forward_refuses(lib, change, word):
     assert _forward(lib, **change) == 1
@@ -50,7 +50,7 @@ def test_forward_refuses(lib, change, word):
 
 
 @pytest.mark.parametrize("change,word", BOTH + [
-    (dict(g=None), b"NULL"), (dict(dX=None, dW=None), b"neither"), (dict(dX=(7 << 32) + 8), b"16"), (dict(lddx=32), b"16"),
+    (dict(g=None), b"NULL"), (dict(g=(6 << 32) + 2), b"4 bytes"), (dict(dX=None, dW=None), b"neither"), (dict(dX=(7 << 32) + 8), b"16"), (dict(lddx=32), b"16"),
     (dict(sdx=0), b"16"), (dict(sdw=64), b"16"), (dict(lddw=65), b"16"), (dict(dX=1 << 32), b"overlap"),
     (dict(dW=(2 << 32) + 1600), b"overlap"), (dict(dW=(7 << 32) + 16), b"overlap"), (dict(dX=6 << 32), b"overlap")])
 def test_backward_refuses(lib, change, word):
