@@ -495,6 +495,12 @@ asap_status asap_xent_backward(int N, int64_t n, int64_t C, int64_t d, int32_t d
                                int64_t lddw, int64_t stride_dw, void* workspace, uint64_t workspace_bytes,
                                void* cuda_stream);
 
+/* Test only: this thread's next asap_xent_forward or asap_xent_backward limits its
+ * waits to wait_ns, and one CTA copies nothing from its tile-th tile on (in the order in
+ * which it takes them) of one kernel -- 0: logits, 1: R, 2: gradients -- so that the
+ * waits for it run out. */
+asap_status asap_debug_xent(int kernel, int tile, uint64_t wait_ns);
+
 /* Bytes of workspace of asap_xent_forward (backward_pass 0) or asap_xent_backward
  * (else): the least, and a good size.  Either may be NULL.  Host only. */
 asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int backward_pass, uint64_t* least,

@@ -56,6 +56,7 @@ SIGNATURES = {
     "asap_mix_noalloc": (C.c_int, [_P, _P, C.c_int, C.c_int64, C.c_int64, _P, _P, C.c_int, _P, _P]),
     "asap_debug_mix_noalloc": (C.c_int, [_P, _P, C.c_int, C.c_int64, C.c_int64, _P, _P, C.c_int, _P, _P, C.c_uint64,
                                          C.c_int64]),
+    "asap_debug_xent": (C.c_int, [C.c_int, C.c_int, C.c_uint64]),
     "asap_xent_workspace": (C.c_int, [C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.POINTER(C.c_uint64),
                                       C.POINTER(C.c_uint64)]),
     "asap_xent_forward": (C.c_int, [C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _P, C.c_int64, C.c_int64, _P,

@@ -106,12 +106,12 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsigned long long limit_ns) {
   if (mbar_try_wait(bar, parity)) return true;
   const unsigned long long t0 = now_ns();
   for (unsigned n = 1;; ++n) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((n & 63u) == 0 && now_ns() - t0 > kWaitNs) return false;
+    if ((n & 63u) == 0 && now_ns() - t0 > limit_ns) return false;
   }
 }
 
@@ -296,6 +296,8 @@ struct Gemm {
   long long acc_rows, ld_acc;
   Out dX, dW;
   int* status;
+  unsigned long long wait_ns;   // a wait's limit
+  int drop;                 // tests: the tile of the first cluster from which its odd CTA loads no more (-1: none)
 };
 
 __device__ __forceinline__ void fail(int* status) { atomicExch(status, static_cast<int>(ASAP_ERR_TIMEOUT)); }
@@ -468,7 +470,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       long long g = 0;
       bool ok = true;
-      while (ok && w.next()) {
+      for (int tile = 0; ok && w.next(); ++tile) {
+        if (tile == a.drop && blockIdx.x == 1) break;
         const CUtensorMap* mx = w.nv == a.n ? &tm_x : &tm_xc;
         const int a0 = w.m * kTile + static_cast<int>(rank) * kHalf;
         const int b0 = (M != kGrads ? a.v0 : 0) + w.nn * kTile + static_cast<int>(rank) * kHalf;
@@ -478,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int worker = w.worker, kt = w.kt;
           for (int k = 0; k < kt; ++k, ++g, ka += kTileK, kb += kTileK) {
             const int s = static_cast<int>(g % kStages);
-            if (g >= kStages && !mbar_wait(empty + s, static_cast<uint32_t>((g / kStages - 1) & 1))) return false;
+            if (g >= kStages && !mbar_wait(empty + s, static_cast<uint32_t>((g / kStages - 1) & 1), a.wait_ns)) return false;
             if (rank == 0) mbar_expect_tx(full + s, 2 * kStageBytes);
             const uint32_t bar = cluster_addr(full + s, 0);
             unsigned char* pa = base + s * kStageBytes;
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // both, as the even CTA's barriers tell; the odd one waits for it at the end.
       if (rank == 0)
         for (int s = 0; s < kStages && s < g; ++s)
-          if (!mbar_wait(full + s, static_cast<uint32_t>(((g - 1 - s) / kStages) & 1))) fail(a.status);
+          if (!mbar_wait(full + s, static_cast<uint32_t>(((g - 1 - s) / kStages) & 1), a.wait_ns)) fail(a.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (ok && w.next()) {
         if (w.kt == 0) continue;
         const int ab = n & 1;
-        if (n >= 2 && !mbar_wait(acc_empty + ab, static_cast<uint32_t>(((n >> 1) - 1) & 1))) {
+        if (n >= 2 && !mbar_wait(acc_empty + ab, static_cast<uint32_t>(((n >> 1) - 1) & 1), a.wait_ns)) {
           fail(a.status);
           break;
         }
@@ -525,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t idesc = instr_desc(a.bf16 != 0, a_mn.value, b_mn.value);
           for (int k = 0; k < w.kt; ++k, ++g) {
             const int s = static_cast<int>(g % kStages);
-            if (!mbar_wait(full + s, static_cast<uint32_t>((g / kStages) & 1))) return false;
+            if (!mbar_wait(full + s, static_cast<uint32_t>((g / kStages) & 1), a.wait_ns)) return false;
             tc_fence_after();
             const uint32_t pa = smem_u32(base + s * kStageBytes), pb = pa + kOperandBytes;
 #pragma unroll
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int ab = n & 1;
       if (w.kt > 0) {
         // All go on or give up together: they meet at barriers.
-        const bool ok = mbar_wait(acc_full + ab, static_cast<uint32_t>((n >> 1) & 1));
+        const bool ok = mbar_wait(acc_full + ab, static_cast<uint32_t>((n >> 1) & 1), a.wait_ns);
         uint32_t bad;
         asm volatile(
             "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
@@ -1103,6 +1106,13 @@ struct Device {
   EncodeTiledFn encode = nullptr;
 };
 
+// Tests: what this thread's next call leaves out (asap_debug_xent).
+struct Drop {
+  int kernel = -1, tile = -1;
+  unsigned long long wait_ns = kWaitNs;
+};
+thread_local Drop t_drop;
+
 constexpr int kMaxDevices = 64;
 std::mutex g_mu;
 Device g_devices[kMaxDevices];
@@ -1305,7 +1315,14 @@ bool meet(const Extent* e, int count, int written) {
   return false;
 }
 
+Drop take_drop() {
+  const Drop d = t_drop;
+  t_drop = Drop();
+  return d;
+}
+
 struct Launch {
+  Drop drop = take_drop();
   cudaStream_t stream;
   bool chained = false;         // a kernel of this call is before it
   cudaLaunchAttribute attr[2];
@@ -1342,7 +1359,10 @@ cudaError_t launch_gemm(Launch& l, const Device& dev, const Gemm& a, long long t
                         const CUtensorMap& txc, const CUtensorMap& tw, const CUtensorMap& tr, const CUtensorMap& to1,
                         const CUtensorMap& to2) {
   const int clusters = static_cast<int>(std::min<long long>(tiles, dev.clusters));
-  return cudaLaunchKernelEx(l.at(dim3(2 * clusters), kThreads, kSmemBytes, true), k_xent<M>, tx, txc, tw, tr, to1, to2, a);
+  Gemm b = a;
+  b.wait_ns = l.drop.wait_ns;
+  b.drop = l.drop.kernel == M ? l.drop.tile : -1;
+  return cudaLaunchKernelEx(l.at(dim3(2 * clusters), kThreads, kSmemBytes, true), k_xent<M>, tx, txc, tw, tr, to1, to2, b);
 }
 
 cudaError_t launch_prepare(Launch& l, Prep q) {
@@ -1526,6 +1546,15 @@ extern "C" asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t 
   if (!least && !bytes) return reject(ASAP_ERR_ARG, "asap_xent_workspace: NULL pointer");
   if (least) *least = backward_pass ? plan_backward(s, 1).end : plan_forward(s).end;
   if (bytes) *bytes = backward_pass ? plan_backward(s, 0).end : plan_forward(s).end;
+  return ASAP_OK;
+}
+
+extern "C" asap_status asap_debug_xent(int kernel, int tile, uint64_t wait_ns) {
+  if (kernel < kLogits || kernel > kGrads || tile < 0 || wait_ns == 0)
+    return reject(ASAP_ERR_ARG, "asap_debug_xent: need 0 <= kernel <= 2, tile >= 0 and wait_ns > 0");
+  t_drop.kernel = kernel;
+  t_drop.tile = tile;
+  t_drop.wait_ns = wait_ns;
   return ASAP_OK;
 }
 

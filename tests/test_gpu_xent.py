@@ -309,6 +309,37 @@ def test_heads_beyond_32_bit_offsets():
         del z, r, dX, dW
 
 
+@pytest.mark.parametrize("kernel,tile", [(0, 0), (0, 1), (1, 0), (1, 1), (2, 0), (2, 1), (2, 2)])
+@pytest.mark.parametrize("size", ["direct", "splits"])
+def test_a_wait_that_runs_out(kernel, tile, size):
+    # One CTA copies nothing from a tile on: the waits that depend on them end after 20 ms, the results say so, and the
+    # next calls are whole.
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    from paper_1612_08608_gb300._lib import load_library
+    lib = load_library()
+    # the first cluster of 76 has two tiles of logits and of R, and two of dX, then dW's; or three, and one of dX
+    N, n, C, d = (8, 500, 1500, 1280) if size == "direct" else (1, 500, 30000, 512)
+    X, W, y, g = _inputs(N, n, C, d, "bfloat16", seed=kernel, drop=0.1)
+    _, lse = ops.softmax_xent(X, W, y)
+    # (enough for one piece: of a narrow one a cluster would have a tile at most)
+    ws = torch.empty(max(ops.xent_workspace(N, n, C, d, grad=k)[1] for k in (False, True)), dtype=torch.uint8, device="cuda")
+    assert lib.asap_debug_xent(kernel, tile, 20_000_000) == 0
+    if kernel == 0:
+        loss, bad = ops.softmax_xent(X, W, y, workspace=ws)
+        assert bool(torch.isnan(loss[y >= 0]).all()) and bool(torch.isnan(bad[y >= 0]).all())
+    else:
+        dX, dW = ops.softmax_xent_grad(X, W, y, lse, g, workspace=ws)
+        assert bool(torch.isnan(dX).any()) or bool(torch.isnan(dW).any())
+    assert int(ws[:4].view(torch.int32)) == 4                                  # ASAP_ERR_TIMEOUT
+    loss, lse = ops.softmax_xent(X, W, y, workspace=ws)
+    assert int(ws[:4].view(torch.int32)) == 0
+    dX, dW = ops.softmax_xent_grad(X, W, y, lse, g, workspace=ws)
+    assert int(ws[:4].view(torch.int32)) == 0
+    _check(X, W, y, g, loss, lse, dX, dW)
+
+
 def test_streams_and_graphs():
     import torch
 

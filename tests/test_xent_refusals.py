@@ -58,6 +58,11 @@ def test_backward_refuses(lib, change, word):
     assert word in lib.asap_last_error(None)
 
 
+def test_debug_entry_refuses(lib):
+    for bad in ((-1, 0, 1), (3, 0, 1), (0, -1, 1), (0, 0, 0)):
+        assert lib.asap_debug_xent(*bad) == 1 and b"asap_debug_xent" in lib.asap_last_error(None)
+
+
 def test_workspace_sizes(lib):
     least, good = C.c_uint64(), C.c_uint64()
     import random
