@@ -63,7 +63,8 @@ constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                     // a TMA load: 64 x 64 elements
 constexpr uint32_t kOutBytes = kHalf * 32 * 2;                  // a TMA store: 32 columns of 128 rows
 constexpr int kEpiWarps = 16;                                   // four per TMEM lane quarter
-constexpr int kParts = kEpiWarps / 4;                           // parts of a tile's columns, four warps each
+constexpr int kParts = kEpiWarps / 4;                           // parts of a tile's columns, four warps each (with eight
+                                                                // warps dW of 64 rows took 135 us, with sixteen 117)
 constexpr int kPartCols = kTile / kParts;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
@@ -643,7 +644,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (M == kGrads && lane == 0 && warp == 2 && rank == 0) {
             const long long col = static_cast<long long>(w.nn) * kTile;
             if (w.dw) poison(a.dW, w.worker * a.dW.stride + (a.v0 + static_cast<long long>(w.m) * kTile) * a.dW.ld + col, a.bf16);
-            else if (a.direct) poison(a.dX, w.worker * a.dX.stride + static_cast<long long>(a.perm[wn + w.m * kTile]) * a.dX.ld + col, a.bf16);
+            else if (a.direct)
+              poison(a.dX, w.worker * a.dX.stride + static_cast<long long>(a.perm[wn + w.m * kTile]) * a.dX.ld + col, a.bf16);
           }
           break;
         }
@@ -885,11 +887,14 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
 }
 
 // ---- few rows: the loss alone ------------------------------------------------------------
-// One to kFewRows rows (single tokens that are scored) meet the whole head: bound by W's bytes.
+// One row or two (single tokens that are scored) meet the whole head: bound by W's bytes.
 // No tensor core: a warp reads kFewCols rows of W at a time, every lane 16 bytes of each, and
 // multiplies them with X's rows from shared memory in fp32, two products an instruction.
 // Each block leaves a maximum and a sum for each row; nothing has to come before.
-constexpr int kFewRows = 4;
+// A captured forward call, this way and by the tensor cores: 131072 classes of 2048 features, one row 82 us (6.5 TB/s)
+// and 144, two 91 and 147, three 122 and 141, four 138 and 123; 32000 of 128, one 8.7 and 13.3, two 12.0 and 13.0, three
+// 14.5 and 12.5.
+constexpr int kFewRows = 2;
 constexpr int kFewCols = 4;
 constexpr int kFewThreads = 256;
 
@@ -1017,8 +1022,8 @@ constexpr int kLossWarps = 4;
 
 // A warp joins a row's parts.
 __global__ void __launch_bounds__(kLossWarps * 32)
-    k_finish_loss(const float2* part, int slots, const float* zy, const float* zy_sum, const int* perm, const int* nv, const int* y,
-                  int n, int C, float* loss, float* lse, const int* status) {
+    k_finish_loss(const float2* part, int slots, const float* zy, const float* zy_sum, const int* perm, const int* nv,
+                  const int* y, int n, int C, float* loss, float* lse, const int* status) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int worker = blockIdx.y, lane = threadIdx.x & 31, row = blockIdx.x * kLossWarps + (threadIdx.x >> 5);
   const long long wn = static_cast<long long>(worker) * n;
@@ -1189,9 +1194,9 @@ inline long long up(long long v, long long a) { return (v + a - 1) / a * a; }
 constexpr long long kMaxRows = 1 << 24, kMaxVocab = 1 << 28, kMaxD = 1 << 20;
 constexpr int kMaxWorkers = 1024;
 
-// Where everything lies in the workspace, and how the vocabulary is cut.
 constexpr int kFewBlocks = 304;                // of all workers: two on each SM
 
+// Where everything lies in the workspace, and how the vocabulary is cut.
 struct Plan {
   long long n_pad, ldc, ld_acc;
   int tiles_m, tiles_v, tiles_d, splits;
@@ -1206,7 +1211,8 @@ struct Shape {
 };
 
 bool sizes_ok(const Shape& s) {
-  if (!(s.N >= 1 && s.N <= kMaxWorkers && s.n >= 0 && s.n <= kMaxRows && s.C >= 1 && s.C <= kMaxVocab && s.d >= 1 && s.d <= kMaxD))
+  if (!(s.N >= 1 && s.N <= kMaxWorkers && s.n >= 0 && s.n <= kMaxRows && s.C >= 1 && s.C <= kMaxVocab && s.d >= 1 &&
+        s.d <= kMaxD))
     return false;
   // tiles are counted in 32 bits (a split of dX's is at most a cluster's worth more)
   const double m = s.n / 256 + 1, v = static_cast<double>(s.C / 256 + 1), d = static_cast<double>(s.d / 256 + 1);
@@ -1269,7 +1275,8 @@ Plan plan_backward(const Shape& s, size_t bytes) {
   p.piece = whole;
   if (!p.direct) {
     const size_t fixed = end(0, false);
-    if (column) p.piece = static_cast<long long>(std::min(static_cast<size_t>(whole), (bytes > fixed ? bytes - fixed : 0) / column));
+    const size_t left = bytes > fixed ? bytes - fixed : 0;
+    if (column) p.piece = static_cast<long long>(std::min(static_cast<size_t>(whole), left / column));
     p.piece = std::max<long long>(kTile, p.piece / kTile * kTile);
     const long long pieces = (whole + p.piece - 1) / p.piece;
     p.piece = up((whole + pieces - 1) / pieces, kTile);           // all about as wide
@@ -1386,8 +1393,7 @@ cudaError_t forward_few(Launch& l, const Shape& s, bool bf16, const Matrix& X, c
   const int blocks = few_blocks(s);
   const size_t smem = static_cast<size_t>(s.n * up(s.d, 8) * 2);
   cudaLaunchConfig_t* cfg = l.at(dim3(blocks, s.N), kFewThreads, smem, false);
-  cudaError_t e = s.n == 1 ? cudaLaunchKernelEx(cfg, k_few_loss<1>, a) : s.n == 2 ? cudaLaunchKernelEx(cfg, k_few_loss<2>, a)
-                : s.n == 3 ? cudaLaunchKernelEx(cfg, k_few_loss<3>, a) : cudaLaunchKernelEx(cfg, k_few_loss<4>, a);
+  cudaError_t e = s.n == 1 ? cudaLaunchKernelEx(cfg, k_few_loss<1>, a) : cudaLaunchKernelEx(cfg, k_few_loss<2>, a);
   if (e == cudaSuccess)
     e = cudaLaunchKernelEx(l.at(dim3(1, s.N), kLossWarps * 32, 0, false), k_finish_loss, static_cast<const float2*>(part), blocks,
                            static_cast<const float*>(zy), static_cast<const float*>(zy), static_cast<const int*>(nullptr),
@@ -1395,9 +1401,11 @@ cudaError_t forward_few(Launch& l, const Shape& s, bool bf16, const Matrix& X, c
   return e;
 }
 
+#define kSizes                                                                                                    \
+  ": need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256"
 #define XENT_CHECK(f)                                                                                             \
   if (!sizes_ok(s))                                                                                               \
-    return reject(ASAP_ERR_ARG, f ": need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256");       \
+    return reject(ASAP_ERR_ARG, f kSizes);                                                                        \
   if (dtype != ASAP_BF16 && dtype != ASAP_F16) return reject(ASAP_ERR_ARG, f ": need ASAP_BF16 or ASAP_F16");
 
 asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W, const int32_t* y, float* loss, float* lse,
@@ -1449,10 +1457,13 @@ asap_status forward(const Shape& s, int dtype, const Matrix& X, const Matrix& W,
   a.W = static_cast<const uint16_t*>(W.p), a.ldw = W.ld, a.sw = s.N == 1 ? 0 : W.stride;
   a.part = reinterpret_cast<float2*>(w + p.part), a.zy = reinterpret_cast<float*>(w + p.zy), a.status = q.status;
   cudaError_t e = launch_prepare(l, q);
-  if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * p.tiles_v, tx, txc, tw, tw, tw, tw);
+  const long long tiles = static_cast<long long>(s.N) * p.tiles_m * p.tiles_v;
+  const dim3 rows(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N);
+  const float *exact = a.zy, *summed = a.zy + s.N * s.n;
+  if (e == cudaSuccess) e = launch_gemm<kLogits>(l, dev, a, tiles, tx, txc, tw, tw, tw, tw);
   if (e == cudaSuccess)
-    e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>((s.n + kLossWarps - 1) / kLossWarps), s.N), kLossWarps * 32, 0, false), k_finish_loss,
-                           static_cast<const float2*>(a.part), p.tiles_v, static_cast<const float*>(a.zy), static_cast<const float*>(a.zy + s.N * s.n), a.perm, a.nv,
+    e = cudaLaunchKernelEx(l.at(rows, kLossWarps * 32, 0, false), k_finish_loss, static_cast<const float2*>(a.part),
+                           p.tiles_v, exact, summed, a.perm, a.nv,
                            static_cast<const int*>(nullptr), a.n, a.C, loss, lse, static_cast<const int*>(a.status));
   return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_forward: launch failed", e);
 }
@@ -1525,13 +1536,15 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
         !encode(dev, &tro, bf16, w + p.R, a.width, r_rows, s.N, p.piece, p.n_pad * p.piece, true))
       return reject(ASAP_ERR_CUDA, "asap_xent_backward: cuTensorMapEncodeTiled failed");
     a.tiles_v = (a.width + kTile - 1) / kTile;
+    const long long x_tiles = dX.p ? static_cast<long long>(p.tiles_m) * p.splits : 0;
     e = launch_gemm<kResidual>(l, dev, a, static_cast<long long>(s.N) * p.tiles_m * a.tiles_v, tx, txc, tw, tr, tro, tro);
     if (e == cudaSuccess)
-      e = launch_gemm<kGrads>(l, dev, a, static_cast<long long>(s.N) * p.tiles_d * ((dX.p ? static_cast<long long>(p.tiles_m) * p.splits : 0) + (dW.p ? a.tiles_v : 0)),
-                              tx, txc, tw, tr, dW.p ? tdw : tr, dX.p ? tdx : tr);
+      e = launch_gemm<kGrads>(l, dev, a, static_cast<long long>(s.N) * p.tiles_d * (x_tiles + (dW.p ? a.tiles_v : 0)), tx,
+                              txc, tw, tr, dW.p ? tdw : tr, dX.p ? tdx : tr);
   }
+  const dim3 grid(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N);
   if (e == cudaSuccess && dX.p && !p.direct)
-    e = cudaLaunchKernelEx(l.at(dim3(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N), 256, 0, false),
+    e = cudaLaunchKernelEx(l.at(grid, 256, 0, false),
                            k_finish_dx, static_cast<const float*>(a.acc), p.splits, a.N, a.acc_rows, a.ld_acc, a.perm, a.nv,
                            a.scale, a.n, a.d, a.bf16, q.dX, q.lddx, q.sdx, static_cast<const int*>(a.status));
   return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_backward: launch failed", e);
@@ -1542,7 +1555,7 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
 extern "C" asap_status asap_xent_workspace(int N, int64_t n, int64_t C, int64_t d, int backward_pass, uint64_t* least,
                                            uint64_t* bytes) {
   const Shape s = {N, n, C, d};
-  if (!sizes_ok(s)) return reject(ASAP_ERR_ARG, "asap_xent_workspace: need 1 <= N <= 1024, 0 <= n <= 2^24, 1 <= C <= 2^28, 1 <= d <= 2^20, and fewer than 10^9 tiles of 256 x 256");
+  if (!sizes_ok(s)) return reject(ASAP_ERR_ARG, "asap_xent_workspace" kSizes);
   if (!least && !bytes) return reject(ASAP_ERR_ARG, "asap_xent_workspace: NULL pointer");
   if (least) *least = backward_pass ? plan_backward(s, 1).end : plan_forward(s).end;
   if (bytes) *bytes = backward_pass ? plan_backward(s, 0).end : plan_forward(s).end;
