@@ -57,10 +57,25 @@ using namespace asap;
 constexpr int kTile = 256;                     // rows and columns of a cluster's tile
 constexpr int kHalf = 128;                     // of a CTA's share
 constexpr int kTileK = 64;                     // 128 bytes: one swizzle row
-constexpr int kStages = 6;
 constexpr uint32_t kOperandBytes = kHalf * kTileK * 2;          // 16 KB of A, and of B
-constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                     // a TMA load: 64 x 64 elements
+
+// The ring of operand stages: S of them, with A bytes of A and 16 KB of B.  Where no tile has more than 64 rows (logits,
+// residual), A is one box of the even CTA (what the MMA reads behind it is another operand, and comes out in rows that
+// nobody looks at): more of W is on its way, by which such a kernel is bound.  A captured forward call over classes of
+// 2048 features, so and with the six wide stages: 131072 classes, 8 rows 97 us and 124, 32 rows 99 and 100, 64 rows 102
+// and 101; 32000 classes, 8 rows 35 and 40, 64 rows 37 and 37; 32 workers of 1000 classes, 64 rows 43 and 44.
+template <int S, uint32_t A>
+struct Ring {
+  static constexpr int stages = S;
+  static constexpr uint32_t a_bytes = A, bytes = A + kOperandBytes;
+};
+using WideRing = Ring<6, kOperandBytes>;
+using NarrowRing = Ring<8, kBoxBytes>;
+constexpr int kMostStages = NarrowRing::stages;
+constexpr uint32_t kRingBytes = WideRing::stages * WideRing::bytes;
+static_assert(NarrowRing::stages * NarrowRing::bytes <= kRingBytes, "both have the same place");
+
 constexpr uint32_t kOutBytes = kHalf * 32 * 2;                  // a TMA store: 32 columns of 128 rows
 constexpr int kEpiWarps = 16;                                   // four per TMEM lane quarter
 constexpr int kParts = kEpiWarps / 4;                           // parts of a tile's columns, four warps each (with eight
@@ -68,7 +83,7 @@ constexpr int kParts = kEpiWarps / 4;                           // parts of a ti
 constexpr int kPartCols = kTile / kParts;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + kParts * kOutBytes + 256;
+constexpr size_t kSmemBytes = 1024 + kRingBytes + kParts * kOutBytes + 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPairs = 76;                     // clusters that a GB300 holds: what a split is sized for
@@ -420,17 +435,17 @@ __global__ void __launch_bounds__(kThreads, 1)
            const __grid_constant__ CUtensorMap tm_o1, const __grid_constant__ CUtensorMap tm_o2, const Gemm a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  unsigned char* boxes = base + static_cast<size_t>(kStages) * kStageBytes;        // one for each part; logits: the parts' sums
-  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + kParts * kOutBytes);             // [kStages], used in the even CTA
-  uint64_t* empty = full + kStages;
-  uint64_t* acc_full = empty + kStages;                                            // [2]
+  unsigned char* boxes = base + kRingBytes;                                        // one for each part; logits: sums
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + kParts * kOutBytes);             // [kMostStages], used in the even CTA
+  uint64_t* empty = full + kMostStages;
+  uint64_t* acc_full = empty + kMostStages;                                            // [2]
   uint64_t* acc_empty = acc_full + 2;                                              // [2], used in the even CTA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kMostStages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
     }
@@ -467,6 +482,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   least = __reduce_min_sync(0xffffffffu, least);
   Walk<M> w(a, least, most, dead, static_cast<int>(blockIdx.x >> 1), static_cast<int>(gridDim.x >> 1));
 
+  const bool narrow = M != kGrads && most <= 64;
+
   if (warp == 0) {
     if (lane == 0) {
       long long g = 0;
@@ -478,19 +495,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int b0 = (M != kGrads ? a.v0 : 0) + w.nn * kTile + static_cast<int>(rank) * kHalf;
         // Both operands' boxes of a step; which of them have k for their rows is known to the compiler
         // (asked in the loop, with w.dw, a step of dX took 0.50 us, not 0.37).
-        auto steps = [&](const CUtensorMap* ma, const CUtensorMap* mb, int ka, int kb, auto a_mn, auto b_mn) {
+        auto steps = [&](const CUtensorMap* ma, const CUtensorMap* mb, int ka, int kb, auto a_mn, auto b_mn, auto ring) {
+          constexpr int kStages = ring.stages, kBoxesA = ring.a_bytes / kBoxBytes;
+          constexpr uint32_t kBytes = (kBoxesA == 1 ? 1 + 4 : 8) * kBoxBytes;       // of both CTAs
           const int worker = w.worker, kt = w.kt;
           for (int k = 0; k < kt; ++k, ++g, ka += kTileK, kb += kTileK) {
             const int s = static_cast<int>(g % kStages);
             if (g >= kStages && !mbar_wait(empty + s, static_cast<uint32_t>((g / kStages - 1) & 1), a.wait_ns)) return false;
-            if (rank == 0) mbar_expect_tx(full + s, 2 * kStageBytes);
+            if (rank == 0) mbar_expect_tx(full + s, kBytes);
             const uint32_t bar = cluster_addr(full + s, 0);
-            unsigned char* pa = base + s * kStageBytes;
-            unsigned char* pb = pa + kOperandBytes;
+            unsigned char* pa = base + s * ring.bytes;
+            unsigned char* pb = pa + ring.a_bytes;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (a_mn.value) tma_load(pa + h * kBoxBytes, ma, bar, a0 + 64 * h, ka, worker);
-              else tma_load(pa + h * kBoxBytes, ma, bar, ka, a0 + 64 * h, worker);
+              if (kBoxesA == 1 && (h == 1 || rank == 1)) {
+              } else if (a_mn.value) {
+                tma_load(pa + h * kBoxBytes, ma, bar, a0 + 64 * h, ka, worker);
+              } else {
+                tma_load(pa + h * kBoxBytes, ma, bar, ka, a0 + 64 * h, worker);
+              }
               if (b_mn.value) tma_load(pb + h * kBoxBytes, mb, bar, b0 + 64 * h, kb, worker);
               else tma_load(pb + h * kBoxBytes, mb, bar, kb, b0 + 64 * h, worker);
             }
@@ -498,16 +521,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         const int k64 = w.k0 * kTileK;
-        if (M != kGrads) ok = steps(mx, &tm_w, 0, 0, Bool<false>(), Bool<false>());
-        else if (w.dw) ok = steps(&tm_r, mx, 0, 0, Bool<true>(), Bool<true>());
-        else ok = steps(&tm_r, &tm_w, k64, a.v0 + k64, Bool<false>(), Bool<true>());
+        if (narrow) ok = steps(mx, &tm_w, 0, 0, Bool<false>(), Bool<false>(), NarrowRing());
+        else if (M != kGrads) ok = steps(mx, &tm_w, 0, 0, Bool<false>(), Bool<false>(), WideRing());
+        else if (w.dw) ok = steps(&tm_r, mx, 0, 0, Bool<true>(), Bool<true>(), WideRing());
+        else ok = steps(&tm_r, &tm_w, k64, a.v0 + k64, Bool<false>(), Bool<true>(), WideRing());
         if (!ok) fail(a.status);
       }
       // No CTA leaves with a copy in flight: the last one into each stage has landed in
       // both, as the even CTA's barriers tell; the odd one waits for it at the end.
+      const int stages = narrow ? NarrowRing::stages : WideRing::stages;
       if (rank == 0)
-        for (int s = 0; s < kStages && s < g; ++s)
-          if (!mbar_wait(full + s, static_cast<uint32_t>(((g - 1 - s) / kStages) & 1), a.wait_ns)) fail(a.status);
+        for (int s = 0; s < stages && s < g; ++s)
+          if (!mbar_wait(full + s, static_cast<uint32_t>(((g - 1 - s) / stages) & 1), a.wait_ns)) fail(a.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -525,13 +550,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         const uint32_t acc = tmem + static_cast<uint32_t>(ab) * kTile;
         // (what the descriptors hold has to be known to the compiler)
-        auto steps = [&](auto a_mn, auto b_mn) {
+        auto steps = [&](auto a_mn, auto b_mn, auto ring) {
+          constexpr int kStages = ring.stages;
           const uint32_t idesc = instr_desc(a.bf16 != 0, a_mn.value, b_mn.value);
           for (int k = 0; k < w.kt; ++k, ++g) {
             const int s = static_cast<int>(g % kStages);
             if (!mbar_wait(full + s, static_cast<uint32_t>((g / kStages) & 1), a.wait_ns)) return false;
             tc_fence_after();
-            const uint32_t pa = smem_u32(base + s * kStageBytes), pb = pa + kOperandBytes;
+            const uint32_t pa = smem_u32(base + s * ring.bytes), pb = pa + ring.a_bytes;
 #pragma unroll
             for (int kk = 0; kk < kTileK / 16; ++kk)
               umma(acc, smem_desc(pa + kk * (a_mn.value ? 2048 : 32), a_mn.value),
@@ -541,9 +567,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           return true;
         };
-        if (M != kGrads) ok = steps(Bool<false>(), Bool<false>());
-        else if (w.dw) ok = steps(Bool<true>(), Bool<true>());
-        else ok = steps(Bool<false>(), Bool<true>());
+        if (narrow) ok = steps(Bool<false>(), Bool<false>(), NarrowRing());
+        else if (M != kGrads) ok = steps(Bool<false>(), Bool<false>(), WideRing());
+        else if (w.dw) ok = steps(Bool<true>(), Bool<true>(), WideRing());
+        else ok = steps(Bool<false>(), Bool<true>(), WideRing());
         if (!ok) fail(a.status);
         if (ok) {
           umma_commit(cluster_addr(acc_full + ab, 0));
@@ -892,8 +919,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
 // multiplies them with X's rows from shared memory in fp32, two products an instruction.
 // Each block leaves a maximum and a sum for each row; nothing has to come before.
 // A captured forward call, this way and by the tensor cores: 131072 classes of 2048 features, one row 82 us (6.5 TB/s)
-// and 144, two 91 and 147, three 122 and 141, four 138 and 123; 32000 of 128, one 8.7 and 13.3, two 12.0 and 13.0, three
-// 14.5 and 12.5.
+// and 96, two 91 and 96, three 122 and 98; 32000 of 2048, one 27 and 35, two 29 and 36; 32000 of 128, one 10.6 and 12.5,
+// two 13.1 and 12.6; 32 workers of 1000 classes of 256, one 9.0 and 13.3, two 11.4 and 13.1.
 constexpr int kFewRows = 2;
 constexpr int kFewCols = 4;
 constexpr int kFewThreads = 256;
