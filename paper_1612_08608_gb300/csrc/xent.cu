@@ -28,7 +28,8 @@
 // tensor cores' sums are cut off after each step, which shows in the loss (d = 4096,
 // logits of 12: 3e-6 of it); k_finish_loss puts the label's term in lse right by it.
 // R is of the operands' type (an MMA's have one): it is scaled so that the largest |g|
-// comes to lie near the top of fp16's range, on a value that rounding leaves alone.
+// comes to lie near the top of fp16's range, on a value that rounding leaves alone; of few
+// rows it has two terms (kFineRows).
 //
 // Every wait is time-limited.  One that runs out sets the workspace's status word; the
 // kernels after it do nothing but turn their outputs' first element into NaN.
@@ -76,6 +77,13 @@ constexpr int kMostStages = NarrowRing::stages;
 constexpr uint32_t kRingBytes = WideRing::stages * WideRing::bytes;
 static_assert(NarrowRing::stages * NarrowRing::bytes <= kRingBytes, "both have the same place");
 
+// A worker with so few rows with a label has R in two terms: 32 rows of it as rounded, and 32 of what that left
+// out.  Its gradients then take one rounding, that of their own type: with R rounded once, a few rows' errors were 1.4
+// times as large on average and up to 2.8 times, while the roundings of many even out, below 1.5 times.  It costs
+// little, for dX's tiles and dW's steps have 64 rows and more whether R fills them or not: 8 workers of 14 rows and
+// 73972 classes of 48, loss and gradients 280 us with one term and 294 with two.  (64 rows in two terms, 131072 classes
+// of 2048: 438 us, not 418.)
+constexpr int kFineRows = 32;
 constexpr uint32_t kOutBytes = kHalf * 32 * 2;                  // a TMA store: 32 columns of 128 rows
 constexpr int kEpiWarps = 16;                                   // four per TMEM lane quarter
 constexpr int kParts = kEpiWarps / 4;                           // parts of a tile's columns, four warps each (with eight
@@ -252,6 +260,14 @@ __device__ __forceinline__ void join(float& m, float& s, float pm, float ps) {
   if (t > -INFINITY) s = s * ex2((m - t) * kLog2e) + ps * ex2((pm - t) * kLog2e);
   else s += ps;                                                // 0, or NaN
   m = t;
+}
+
+// The same, but what is beyond the type becomes its largest value.
+__device__ __forceinline__ uint32_t pack16_finite(float lo, float hi, bool bf16) {
+  uint32_t u;
+  if (bf16) asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+  return u;
 }
 
 __device__ __forceinline__ float2 unpack16(uint32_t u, bool bf16) {
@@ -490,7 +506,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int tile = 0; ok && w.next(); ++tile) {
         if (tile == a.drop && blockIdx.x == 1) break;
-        const CUtensorMap* mx = w.nv == a.n ? &tm_x : &tm_xc;
+        const bool twice = M != kLogits && w.nv <= kFineRows;   // X's rows, for R's two terms
+        const CUtensorMap* mx = w.nv == a.n && !twice ? &tm_x : &tm_xc;
         const int a0 = w.m * kTile + static_cast<int>(rank) * kHalf;
         const int b0 = (M != kGrads ? a.v0 : 0) + w.nn * kTile + static_cast<int>(rank) * kHalf;
         // Both operands' boxes of a step; which of them have k for their rows is known to the compiler
@@ -607,6 +624,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
       }
     };
+    // The second term's rows of dX, 32 on, to the first's.
+    auto join_fine = [&] {
+      if (chief) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      part_sync();
+      float4* sums = reinterpret_cast<float4*>(box) + lane * 8;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (quarter == 1) sums[q ^ (r & 7)] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+      part_sync();
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (quarter == 0) {
+          const float4 t = sums[q ^ (r & 7)];
+          v[4 * q] += t.x;
+          v[4 * q + 1] += t.y;
+          v[4 * q + 2] += t.z;
+          v[4 * q + 3] += t.w;
+        }
+    };
     // The first `left` of the 32 columns to this thread's own row (at a multiple of 16 bytes).
     auto to_row = [&](uint16_t* o, int left) {
 #pragma unroll
@@ -631,7 +667,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int row = w.m * kTile + static_cast<int>(rank) * kHalf + r;   // of the tile's matrix
       const int col0 = w.nn * kTile + part * kPartCols;                   // this thread's first column
       const long long wn = static_cast<long long>(w.worker) * a.n;
-      const bool live = !w.dw && row < w.nv;
+      // R's second term: its rows meet the same rows of X.
+      const bool second = M == kResidual && w.nv <= kFineRows && row >= kFineRows && row < 2 * kFineRows;
+      const int item = second ? row - kFineRows : row;
+      const bool live = !w.dw && item < w.nv;
       if (M != kLogits && w.worker != seen) {
         seen = w.worker;
         scale = a.scale[seen];
@@ -640,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // What a row needs is fetched while its products are still summed.
       int at = 0, yb = -1;
       float off = 0.f, gs = 0.f;
-      if (live && (M != kGrads || a.direct)) at = a.perm[wn + row];
+      if (live && (M != kGrads || a.direct)) at = a.perm[wn + item];
       if (live && M != kGrads) yb = a.y[wn + at] - a.v0;
       if (live && M == kResidual) {
         off = -a.lse[wn + at] * kLog2e;
@@ -731,57 +770,75 @@ __global__ void __launch_bounds__(kThreads, 1)
           a.part[(wn + row) * a.tiles_v + w.nn] = make_float2(m, s);
         }
       } else if (M == kResidual) {
-        for (int c = 0; c < kPartCols / 32; ++c) {
-          const int cc = col0 + 32 * c;
-          if (cc >= a.width) break;
-          tmem_ld32(trow + 32 * c, v);
+        auto drain = [&](auto fine) {
+          for (int c = 0; c < kPartCols / 32; ++c) {
+            const int cc = col0 + 32 * c;
+            if (cc >= a.width) break;
+            tmem_ld32(trow + 32 * c, v);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p = ex2(fmaf(v[j], kLog2e, off)) - (cc + j == yb ? 1.f : 0.f);
-            v[j] = live && cc + j < a.width ? gs * p : 0.f;
+            for (int j = 0; j < 32; ++j) {
+              const float p = ex2(fmaf(v[j], kLog2e, off)) - (cc + j == yb ? 1.f : 0.f);
+              v[j] = live && cc + j < a.width ? gs * p : 0.f;
+            }
+            if (fine.value && second) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float2 h = unpack16(pack16_finite(v[j], v[j + 1], a.bf16), a.bf16);
+                v[j] -= h.x;                                    // (of infinity infinity is left, not NaN)
+                v[j + 1] -= h.y;
+              }
+            }
+            to_box(&tm_o1, cc, row - r, w.worker, w.nv);
           }
-          to_box(&tm_o1, cc, row - r, w.worker, w.nv);
-        }
+        };
+        if (w.nv <= kFineRows) drain(Bool<true>());
+        else drain(Bool<false>());
       } else {
         // dX's rows go one by one where some are left out; so does a row's end that is no
         // multiple of 16 bytes: a TMA store writes whole groups of them.
         const bool sums = !w.dw && !a.direct, together = w.dw || w.nv == a.n;
+        const bool fine = !w.dw && w.nv <= kFineRows;           // (its sums go on in two terms)
         const bool stored = w.dw ? a.v0 + row < a.C : live;
-        for (int c = 0; c < kPartCols / 32; ++c) {
-          const int cc = col0 + 32 * c;
-          if (cc >= a.d) break;
-          if (w.kt > 0) {
-            tmem_ld32(trow + 32 * c, v);
-          } else {
+        auto drain = [&](auto terms) {
+          for (int c = 0; c < kPartCols / 32; ++c) {
+            const int cc = col0 + 32 * c;
+            if (cc >= a.d) break;
+            if (w.kt > 0) {
+              tmem_ld32(trow + 32 * c, v);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0.f;
-          }
-          if (!sums) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] *= unscale;
-            if (together && (cc + 32 <= a.d || (a.d & 7) == 0)) {
-              if (w.dw) to_box(&tm_o1, cc, a.v0 + row - r, w.worker, a.C);
-              else to_box(&tm_o2, cc, row - r, w.worker, a.n);
-            } else if (stored) {
-              const Out& out = w.dw ? a.dW : a.dX;
-              to_row(out.p + w.worker * out.stride + (w.dw ? a.v0 + static_cast<long long>(row) : at) * out.ld + cc, a.d - cc);
+              for (int j = 0; j < 32; ++j) v[j] = 0.f;
             }
-            continue;
-          }
-          if (!stored) continue;
-          float* o = a.acc + ((static_cast<long long>(w.split) * a.N + w.worker) * a.acc_rows + row) * a.ld_acc + cc;
+            if (!sums) {
+              if (terms.value) join_fine();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (cc + 8 * q >= a.ld_acc) break;
-            if (!a.first) {
-              float p[8];
-              ld_global8(o + 8 * q, p);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[8 * q + e] += p[e];
+              for (int j = 0; j < 32; ++j) v[j] *= unscale;
+              if (together && (cc + 32 <= a.d || (a.d & 7) == 0)) {
+                if (w.dw) to_box(&tm_o1, cc, a.v0 + row - r, w.worker, a.C);
+                else to_box(&tm_o2, cc, row - r, w.worker, a.n);
+              } else if (stored) {
+                const Out& out = w.dw ? a.dW : a.dX;
+                to_row(out.p + w.worker * out.stride + (w.dw ? a.v0 + static_cast<long long>(row) : at) * out.ld + cc, a.d - cc);
+              }
+              continue;
             }
-            st_global8(o + 8 * q, v + 8 * q);
+            if (!stored && !(terms.value && row >= kFineRows && row < kFineRows + w.nv)) continue;
+            float* o = a.acc + ((static_cast<long long>(w.split) * a.N + w.worker) * a.acc_rows + row) * a.ld_acc + cc;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (cc + 8 * q >= a.ld_acc) break;
+              if (!a.first) {
+                float p[8];
+                ld_global8(o + 8 * q, p);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[8 * q + e] += p[e];
+              }
+              st_global8(o + 8 * q, v + 8 * q);
+            }
           }
-        }
+        };
+        if (fine) drain(Bool<true>());
+        else drain(Bool<false>());
       }
       if (w.kt > 0) {
         release_acc();
@@ -858,6 +915,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
     first += s_before[w];
     top = fmaxf(top, s_max[w]);
   }
+  const bool twice = g && nv <= kFineRows;                      // for R's two terms
   if (blockIdx.x == 0 && tid == 0) {
     a.nv[worker] = nv;
     // The largest |g| becomes the largest value below 2^14 that R's type holds: what has no
@@ -895,8 +953,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
         continue;
       }
       const uint16_t* x = a.X + worker * a.sx + (r0 + q) * a.ldx;
-      if (nv < a.n) {
-        uint16_t* dst = a.Xc + (worker * a.rows + at) * a.ldc;
+      for (int copy = 0; copy < (twice ? 2 : nv < a.n ? 1 : 0); ++copy) {
+        uint16_t* dst = a.Xc + (worker * a.rows + at + copy * kFineRows) * a.ldc;
 #pragma unroll 4
         for (int v = lane; v < a.d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = reinterpret_cast<const uint4*>(x)[v];
         const int c = a.d / 8 * 8 + lane;
@@ -906,10 +964,11 @@ __global__ void __launch_bounds__(kPrepThreads) k_prepare(const Prep a) {
     first += __popc(rows_in);
   }
   // what a last step of 64 rows reads beyond the rows that were copied
-  if (nv < a.n && blockIdx.x == gridDim.x - 1)
+  if ((nv < a.n || twice) && blockIdx.x == gridDim.x - 1)
     for (int q = nv + warp; q < (nv + kTileK - 1) / kTileK * kTileK; q += kPrepThreads / 32) {
+      if (twice && q >= kFineRows && q < kFineRows + nv) continue;
       uint16_t* dst = a.Xc + (worker * a.rows + q) * a.ldc;
-      for (int c = lane; c < a.d; c += 32) dst[c] = 0;
+      for (int v = lane; v < a.ldc / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
@@ -1085,28 +1144,52 @@ __global__ void __launch_bounds__(kLossWarps * 32)
   loss[wn + at] = l - z;
 }
 
-// dX of the rows with a label from the splits' sums.
-__global__ void __launch_bounds__(256)
-    k_finish_dx(const float* acc, int splits, int N, long long rows, long long ld, const int* perm, const int* nv,
+// dX of the rows with a label from the splits' sums: a warp for 128 columns of a row, or, where there are many splits,
+// eight, which take every eighth of them (76 splits of 2 rows in two terms: 32 us and 8; 9 splits of 14: 13 and 5; one split of 4096
+// rows takes 47 us by one warp).
+constexpr int kDxWarps = 8;
+
+__global__ void __launch_bounds__(kDxWarps * 32)
+    k_finish_dx(const float* acc, int splits, int ways, int N, long long rows, long long ld, const int* perm, const int* nv,
                 const float* scale, int n, int d, int bf16, uint16_t* dX, long long lddx, long long sdx, const int* status) {
+  __shared__ float4 s_sum[kDxWarps][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int worker = blockIdx.z;
+  const int worker = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (*static_cast<const volatile int*>(status) != 0) {
     if (blockIdx.x == 0 && blockIdx.y == 0 && worker == 0 && threadIdx.x == 0) dX[0] = bf16 ? 0x7fc0 : 0x7e00;
     return;
   }
   const float unscale = 1.f / scale[worker];
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4;
-  if (c >= d) return;
-  for (int row = blockIdx.x; row < nv[worker]; row += gridDim.x) {
+  const int rows_in = nv[worker], terms = rows_in <= kFineRows ? 2 : 1;
+  const int c = (blockIdx.y * 32 + lane) * 4, way = warp % ways, per = kDxWarps / ways;
+  for (int row0 = blockIdx.x * per; row0 < rows_in; row0 += gridDim.x * per) {
+    const int row = row0 + warp / ways;
+    const bool in = row < rows_in && c < d;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < splits; ++s) {
-      const float4 p = *reinterpret_cast<const float4*>(acc + ((static_cast<long long>(s) * N + worker) * rows + row) * ld + c);
-      x.x += p.x;
-      x.y += p.y;
-      x.z += p.z;
-      x.w += p.w;
+    for (int term = 0; in && term < terms; ++term) {
+      const float* at = acc + (worker * rows + row + term * kFineRows) * ld + c;
+#pragma unroll 4
+      for (int s = way; s < splits; s += ways) {
+        const float4 p = *reinterpret_cast<const float4*>(at + s * (N * rows * ld));
+        x.x += p.x;
+        x.y += p.y;
+        x.z += p.z;
+        x.w += p.w;
+      }
     }
+    if (ways > 1) {
+      s_sum[warp][lane] = x;
+      __syncthreads();
+      for (int q = 1; way == 0 && q < ways; ++q) {
+        const float4 p = s_sum[warp + q][lane];
+        x.x += p.x;
+        x.y += p.y;
+        x.z += p.z;
+        x.w += p.w;
+      }
+      __syncthreads();
+    }
+    if (way != 0 || !in) continue;
     uint16_t* o = dX + worker * sdx + static_cast<long long>(perm[static_cast<long long>(worker) * n + row]) * lddx + c;
     const uint2 q = make_uint2(pack16(x.x * unscale, x.y * unscale, bf16), pack16(x.z * unscale, x.w * unscale, bf16));
     if (c + 4 <= d) *reinterpret_cast<uint2*>(o) = q;            // rows start at multiples of 16 bytes
@@ -1569,10 +1652,12 @@ asap_status backward(const Shape& s, int dtype, const Matrix& X, const Matrix& W
       e = launch_gemm<kGrads>(l, dev, a, static_cast<long long>(s.N) * p.tiles_d * (x_tiles + (dW.p ? a.tiles_v : 0)), tx,
                               txc, tw, tr, dW.p ? tdw : tr, dX.p ? tdx : tr);
   }
-  const dim3 grid(static_cast<unsigned>(std::min<long long>(s.n, 2048)), static_cast<unsigned>((s.d + 1023) / 1024), s.N);
+  const int ways = p.splits >= kDxWarps ? kDxWarps : 1;
+  const dim3 grid(static_cast<unsigned>(std::min<long long>(up(s.n * ways, kDxWarps) / kDxWarps, 2048)),
+                  static_cast<unsigned>((s.d + 127) / 128), s.N);
   if (e == cudaSuccess && dX.p && !p.direct)
-    e = cudaLaunchKernelEx(l.at(grid, 256, 0, false),
-                           k_finish_dx, static_cast<const float*>(a.acc), p.splits, a.N, a.acc_rows, a.ld_acc, a.perm, a.nv,
+    e = cudaLaunchKernelEx(l.at(grid, kDxWarps * 32, 0, false),
+                           k_finish_dx, static_cast<const float*>(a.acc), p.splits, ways, a.N, a.acc_rows, a.ld_acc, a.perm, a.nv,
                            a.scale, a.n, a.d, a.bf16, q.dX, q.lddx, q.sdx, static_cast<const int*>(a.status));
   return e == cudaSuccess ? ASAP_OK : launch_error("asap_xent_backward: launch failed", e);
 }
