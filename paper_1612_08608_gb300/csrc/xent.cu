@@ -90,6 +90,7 @@ constexpr int kParts = kEpiWarps / 4;                           // parts of a ti
                                                                 // warps dW of 64 rows took 135 us, with sixteen 117)
 constexpr int kPartCols = kTile / kParts;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr int kLongSum = 1024;                                  // features
 constexpr uint32_t kTmemCols = 512;                             // two accumulators of 256
 constexpr size_t kSmemBytes = 1024 + kRingBytes + kParts * kOutBytes + 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
@@ -499,6 +500,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   Walk<M> w(a, least, most, dead, static_cast<int>(blockIdx.x >> 1), static_cast<int>(gridDim.x >> 1));
 
   const bool narrow = M != kGrads && most <= 64;
+  // A cluster with one tile has an accumulator to spare: of long sums, which the tensor cores cut off after each step,
+  // it takes every other 64 (800 rows, 10 classes of 4096 features: loss off by 8.7e-7 of it in bf16, in one sum 1.7e-6).
+  const bool spare = M == kLogits && w.end <= w.clusters && a.d >= kLongSum;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         const uint32_t acc = tmem + static_cast<uint32_t>(ab) * kTile;
         // (what the descriptors hold has to be known to the compiler)
-        auto steps = [&](auto a_mn, auto b_mn, auto ring) {
+        auto steps = [&](auto a_mn, auto b_mn, auto ring, auto both) {
           constexpr int kStages = ring.stages;
           const uint32_t idesc = instr_desc(a.bf16 != 0, a_mn.value, b_mn.value);
           for (int k = 0; k < w.kt; ++k, ++g) {
@@ -577,17 +581,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t pa = smem_u32(base + s * ring.bytes), pb = pa + ring.a_bytes;
 #pragma unroll
             for (int kk = 0; kk < kTileK / 16; ++kk)
-              umma(acc, smem_desc(pa + kk * (a_mn.value ? 2048 : 32), a_mn.value),
-                   smem_desc(pb + kk * (b_mn.value ? 2048 : 32), b_mn.value), idesc, (k | kk) != 0);
+              umma(acc + (both.value ? (k & 1) * kTile : 0), smem_desc(pa + kk * (a_mn.value ? 2048 : 32), a_mn.value),
+                   smem_desc(pb + kk * (b_mn.value ? 2048 : 32), b_mn.value), idesc, ((both.value ? k >> 1 : k) | kk) != 0);
             umma_commit(cluster_addr(empty + s, 0));
             umma_commit(cluster_addr(empty + s, 1));
           }
           return true;
         };
-        if (narrow) ok = steps(Bool<false>(), Bool<false>(), NarrowRing());
-        else if (M != kGrads) ok = steps(Bool<false>(), Bool<false>(), WideRing());
-        else if (w.dw) ok = steps(Bool<true>(), Bool<true>(), WideRing());
-        else ok = steps(Bool<false>(), Bool<true>(), WideRing());
+        if (spare && narrow) ok = steps(Bool<false>(), Bool<false>(), NarrowRing(), Bool<M == kLogits>());
+        else if (spare) ok = steps(Bool<false>(), Bool<false>(), WideRing(), Bool<M == kLogits>());
+        else if (narrow) ok = steps(Bool<false>(), Bool<false>(), NarrowRing(), Bool<false>());
+        else if (M != kGrads) ok = steps(Bool<false>(), Bool<false>(), WideRing(), Bool<false>());
+        else if (w.dw) ok = steps(Bool<true>(), Bool<true>(), WideRing(), Bool<false>());
+        else ok = steps(Bool<false>(), Bool<true>(), WideRing(), Bool<false>());
         if (!ok) fail(a.status);
         if (ok) {
           umma_commit(cluster_addr(acc_full + ab, 0));
@@ -722,39 +728,49 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (M == kLogits) {
         float m = -INFINITY, s = 0.f, zy = 0.f;
         bool mine = false;
-        for (int c = 0; c < kPartCols / 32; ++c) {
-          const int cc = col0 + 32 * c;
-          if (cc >= a.C) break;
-          tmem_ld32(trow + 32 * c, v);
-          if (cc + 32 > a.C) {
+        auto drain = [&](auto both) {
+          for (int c = 0; c < kPartCols / 32; ++c) {
+            const int cc = col0 + 32 * c;
+            if (cc >= a.C) break;
+            tmem_ld32(trow + 32 * c, v);
+            if (both.value) {
+              float u[32];
+              tmem_ld32(trow + kTile + 32 * c, u);
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (cc + j >= a.C) v[j] = -INFINITY;
+              for (int j = 0; j < 32; ++j) v[j] += u[j];
+            }
+            if (cc + 32 > a.C) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (cc + j >= a.C) v[j] = -INFINITY;
+            }
+            if (yb >= cc && yb < cc + 32) {
+              mine = true;
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (cc + j == yb) zy = v[j];
+            }
+            float cm = m;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) cm = fmaxf(cm, v[j]);
+            // Nothing but -inf so far adds nothing; NaN goes on in the sum.
+            const float mm = cm == -INFINITY ? 0.f : cm;
+            const float top = -mm * kLog2e;
+            s *= ex2(fmaf(m, kLog2e, top));
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              s0 += ex2(fmaf(v[j], kLog2e, top));
+              s1 += ex2(fmaf(v[j + 1], kLog2e, top));
+              s2 += ex2(fmaf(v[j + 2], kLog2e, top));
+              s3 += ex2(fmaf(v[j + 3], kLog2e, top));
+            }
+            s += (s0 + s1) + (s2 + s3);
+            m = cm;
           }
-          if (yb >= cc && yb < cc + 32) {
-            mine = true;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (cc + j == yb) zy = v[j];
-          }
-          float cm = m;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) cm = fmaxf(cm, v[j]);
-          // Nothing but -inf so far adds nothing; NaN goes on in the sum.
-          const float mm = cm == -INFINITY ? 0.f : cm;
-          const float top = -mm * kLog2e;
-          s *= ex2(fmaf(m, kLog2e, top));
-          float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            s0 += ex2(fmaf(v[j], kLog2e, top));
-            s1 += ex2(fmaf(v[j + 1], kLog2e, top));
-            s2 += ex2(fmaf(v[j + 2], kLog2e, top));
-            s3 += ex2(fmaf(v[j + 3], kLog2e, top));
-          }
-          s += (s0 + s1) + (s2 + s3);
-          m = cm;
-        }
+        };
+        if (spare) drain(Bool<true>());
+        else drain(Bool<false>());
         if (mine) a.zy[static_cast<long long>(a.N) * a.n + wn + row] = zy;
         // The parts' sums meet in shared memory (that of a tile and the next in turn: who is
         // still joining one has yet to come to the other's barrier).

@@ -365,6 +365,26 @@ def test_short_tiles(N, n, C, d, dtype):
     _check(X, W, y, g, *_run(X, W, y, g, workspace=ws), few=True)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("N,n,C,d", [(1, 800, 10, 4096), (1, 40, 50, 4090), (6, 300, 300, 1024), (1, 300, 9500, 1100), (2, 3, 14, 2056),
+                                     (1, 300, 9800, 1100), (1, 6, 10, 1023)])
+def test_long_sums_of_few_classes(N, n, C, d, dtype):
+    # Where a cluster has one tile at most, sums over 1024 features and more come in two parts; 9800 classes are too many.
+    import torch
+    X, W, y, g = _inputs(N, n, C, d, dtype, seed=C + d, drop=0.2)
+    loss, lse, dX, dW = _run(X, W, y, g)
+    _check(X, W, y, g, loss, lse, dX, dW)
+    if d >= 1024 and C < 9800:
+        # 2^-23 of a sum lost by a step is what _check allows to both parts together: here to each, over half the steps
+        for i in range(N):
+            rows = torch.nonzero(y[i] >= 0).flatten()
+            x, w = X[i][rows].double(), W[i].double()
+            z = x @ w.T
+            want = torch.logsumexp(z, dim=1)
+            tl = (d / 32 + 8) * 2.0 ** -23 * float((x.abs() @ w.abs().T).max()) + 2.0 ** -21 * (want.abs() + 1)
+            assert bool(((lse[i][rows] - want).abs() <= tl).all())
+
+
 @pytest.mark.parametrize("kernel,tile", [(0, 0), (0, 1), (1, 0), (1, 1)])
 def test_a_wait_that_runs_out_in_short_tiles(kernel, tile):
     # as above; each of 76 clusters has two tiles or three, of twelve steps
