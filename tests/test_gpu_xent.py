@@ -366,8 +366,8 @@ def test_short_tiles(N, n, C, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("N,n,C,d", [(1, 800, 10, 4096), (1, 40, 50, 4090), (6, 300, 300, 1024), (1, 300, 9500, 1100), (2, 3, 14, 2056),
-                                     (1, 300, 9800, 1100), (1, 6, 10, 1023)])
+@pytest.mark.parametrize("N,n,C,d", [(1, 800, 10, 4096), (1, 40, 50, 4090), (6, 300, 300, 1024), (1, 300, 9500, 1100),
+                                     (2, 3, 14, 2056), (1, 300, 9800, 1100), (1, 6, 10, 1023)])
 def test_long_sums_of_few_classes(N, n, C, d, dtype):
     # Where a cluster has one tile at most, sums over 1024 features and more come in two parts; 9800 classes are too many.
     import torch
@@ -383,6 +383,42 @@ def test_long_sums_of_few_classes(N, n, C, d, dtype):
             want = torch.logsumexp(z, dim=1)
             tl = (d / 32 + 8) * 2.0 ** -23 * float((x.abs() @ w.abs().T).max()) + 2.0 ** -21 * (want.abs() + 1)
             assert bool(((lse[i][rows] - want).abs() <= tl).all())
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("N,n,C,d,top", [(1, 5, 300, 32768, 10.0), (1, 5, 300, 32768, 14.0), (2, 70, 300, 16384, 10.0),
+                                         (1, 20, 20000, 4096, 15.0), (3, 2, 28, 3984, 9.0)])
+def test_confident_rows(N, n, C, d, top, dtype):
+    # What is left of 1 of a label's probability comes from its logit as fp32 arithmetic gives it: a lane sums d / 256 groups
+    # of eight products, 32 lanes join in five steps, each off by 2^-24 of the magnitudes' sum S.
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    X, W, y, g = _inputs(N, n, C, d, dtype, seed=d + n, label=0.0)
+    X.copy_((W[torch.arange(N, device="cuda")[:, None], y.long()].float() * top).to(X.dtype))
+    loss, lse = ops.softmax_xent(X, W, y)
+    dX, dW = ops.softmax_xent_grad(X, W, y, lse, g)
+    _check(X, W, y, g, loss, lse, dX, dW)
+    eps = torch.finfo(X.dtype).eps
+    tiny = 2.0 ** -25 if X.dtype == torch.float16 else 0.0
+    for i in range(N):
+        x, w, at = X[i].double(), W[i].double(), torch.arange(n, device="cuda")
+        z, S, yy = x @ w.T, x.abs() @ w.abs().T, y[i].long()
+        p = torch.exp(z - lse[i].double()[:, None])
+        hot = torch.zeros_like(p)
+        hot[at, yy] = 1.0
+        gg = g[i].double()[:, None]
+        half = eps * eps / 4 if n <= 32 else eps / 2
+        off = p * (3 * (d / 16 + 8) * 2.0 ** -23 * S.max() + half + 2.0 ** -20)
+        py = p[at, yy]
+        off[at, yy] = 1.5 * py * (d / 256 + 9) * 2.0 ** -24 * S[at, yy] + (half + 2.0 ** -22) * (1 - py).abs()
+        off, R = gg.abs() * off, gg * (p - hot)
+        small = float(gg.abs().max()) * 2.0 ** -38 if X.dtype == torch.float16 else 0.0
+        for got, want, mag, err, sums in ((dX[i], R @ w, R.abs() @ w.abs(), off @ w.abs() + small * w.abs().sum(dim=0), C),
+                                          (dW[i], R.T @ x, R.abs().T @ x.abs(),
+                                           off.T @ x.abs() + small * x.abs().sum(dim=0), n)):
+            tol = err + (sums / 16 + 16) * 2.0 ** -23 * mag + eps / 2 * want.abs() + tiny
+            assert bool(((got - want).abs() <= tol).all()), ((got - want).abs() / tol).max()
 
 
 @pytest.mark.parametrize("kernel,tile", [(0, 0), (0, 1), (1, 0), (1, 1)])
