@@ -760,15 +760,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 32; ++j) cm = fmaxf(cm, v[j]);
             // Nothing but -inf so far adds nothing; NaN goes on in the sum.
             const float mm = cm == -INFINITY ? 0.f : cm;
-            const float top = -mm * kLog2e;
-            s *= ex2(fmaf(m, kLog2e, top));
+            // The largest's own term has to be 1: of a confident row the others' are what the loss is.  (By fma with
+            // -m log2(e), as rounded, it is off by up to 2^-24 of that; 4095 rows: 380 us so, 384 with the difference.)
+            s *= ex2((m - mm) * kLog2e);
             float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
-              s0 += ex2(fmaf(v[j], kLog2e, top));
-              s1 += ex2(fmaf(v[j + 1], kLog2e, top));
-              s2 += ex2(fmaf(v[j + 2], kLog2e, top));
-              s3 += ex2(fmaf(v[j + 3], kLog2e, top));
+              s0 += ex2((v[j] - mm) * kLog2e);
+              s1 += ex2((v[j + 1] - mm) * kLog2e);
+              s2 += ex2((v[j + 2] - mm) * kLog2e);
+              s3 += ex2((v[j + 3] - mm) * kLog2e);
             }
             s += (s0 + s1) + (s2 + s3);
             m = cm;

@@ -385,6 +385,26 @@ def test_long_sums_of_few_classes(N, n, C, d, dtype):
             assert bool(((lse[i][rows] - want).abs() <= tl).all())
 
 
+@pytest.mark.parametrize("n", [1, 2, 5, 40, 300])
+@pytest.mark.parametrize("top", [50.25, 100.5, 129.0, 201.0])
+def test_a_certain_row_has_no_loss(n, top):
+    # The label's logit is one product, the others' are 0, and e^-50 is nothing beside 1: no rounding is left.
+    import torch
+
+    from paper_1612_08608_gb300 import ops
+    C, d = 300, 64
+    W = torch.zeros((1, C, d), device="cuda", dtype=torch.bfloat16)
+    W[0, torch.arange(d), torch.arange(d)] = 1.0
+    y = (torch.arange(n, device="cuda", dtype=torch.int32) * 7 % d)[None]
+    X = torch.zeros((1, n, d), device="cuda", dtype=torch.bfloat16)
+    X[0, torch.arange(n, device="cuda"), y[0].long()] = top
+    loss, lse = ops.softmax_xent(X, W, y)
+    assert bool((loss == 0).all()) and bool((lse == X.float().amax(dim=2)).all())
+    dX, dW = ops.softmax_xent_grad(X, W, y, lse, torch.ones_like(loss))
+    tiny = 300 * top * 2.0 ** -72                               # e^-50 < 2^-72
+    assert bool((dX.abs() <= tiny).all()) and bool((dW.abs() <= n * tiny).all())
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("N,n,C,d,top", [(1, 5, 300, 32768, 10.0), (1, 5, 300, 32768, 14.0), (2, 70, 300, 16384, 10.0),
                                          (1, 20, 20000, 4096, 15.0), (3, 2, 28, 3984, 9.0)])
