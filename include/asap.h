@@ -483,8 +483,8 @@ asap_status asap_xent_forward(int N, int64_t n, int64_t C, int64_t d, int32_t dt
  * vocabulary at a time: R of one piece is held in the workspace, scaled so
  * that the largest |g| of a worker lies at 2^14, and rounded to `dtype`; so an
  * element of dX or dW is off by about one rounding of R's elements and one of its
- * own.  dX rows of rows left out, and of those with
- * y >= C, are 0.  A workspace of `least` bytes takes pieces
+ * own; of a worker with 32 labels or fewer R is kept in two terms, which leaves the
+ * latter.  dX rows of rows left out, and of those with y >= C, are 0.  A workspace of `least` bytes takes pieces
  * of 256 columns; more makes them wider, and fewer (asap_xent_workspace's `bytes`
  * is a good size; the width changes the order of dX's sums).  If a wait runs out,
  * dX and dW hold a NaN and the workspace's first int32 is ASAP_ERR_TIMEOUT.  The rest
